@@ -1,0 +1,767 @@
+// Attention of whole prompts under score rules.  Queries and keys of a prompt
+// meet on the matrix cores (v_mfma_f32_32x32x16_f16, fp32 sums) one tile of 32
+// keys x 32 queries at a time, in one pass over the keys with a running maximum
+// and sum per query:
+//   S^T = K Q^T        keys along the tile's rows, queries along its columns
+//   P^T = exp2(S^T - m)
+//   O^T += V^T P^T
+// so a lane holds one query of a tile: its statistics are scalars, and the
+// sixteen weights that it computes are, rounded to fp16, the right operand of
+// the value product without leaving their registers (the order of the keys in
+// that product's reduction is the one they come out in; V^T is read from LDS
+// with the transposing loads in the same order).
+//
+// A wave holds 64 queries (two tiles) of one query head; a block's four waves
+// stream the same K and V rows through LDS.  One wave per SIMD: the output
+// tiles take 128 registers, the queries 64, and every operand read from LDS
+// serves two MFMAs, which halves the LDS traffic that 32 queries per wave would
+// need (all of its bandwidth).  The MFMAs of one half step, the logits of the
+// next tile and the value product of the one before, run beside the
+// exponentials of the tile between them (stage).
+//
+// Every query sees the keys of one interval; a tile that lies inside it for all
+// 32 queries takes the plain path, others are masked first.
+#include <algorithm>
+
+#include "../../include/mikv_layer.h"
+#include "prompt_device.h"
+
+namespace mikv {
+
+namespace {
+
+constexpr int kTileKeys = 64;           // keys per LDS tile
+constexpr int kBlockRows = 4 * kWaveRows;
+constexpr float kRaise = 1024.0f;       // raise a query's maximum when a lane's 16 weights of a tile sum past this
+constexpr float kInf = __builtin_huge_valf();
+
+struct PromptArgs {
+  const uint16_t *q, *k, *v;
+  int64_t qs[3], ks[3], vs[3], os[3];
+  uint16_t *out;
+  float *lse;
+  const float *slopes;
+  const int32_t *begin, *end;
+  int q_heads, kv_heads, units, nblk, run, T;
+  float scale, cap;  // scale: of the logit in log2 units (cap: to the argument of tanh); cap in log2 units
+};
+
+typedef int16_t s4_t __attribute__((ext_vector_type(4)));
+
+// The rows of a streamed tile straight to LDS (each wave instruction moves four
+// rows), zeros past the prompt.  SWZ(row) is XORed into a row's 16-byte word index.
+template <class Swz>
+__device__ inline void stage_rows(u4_t *lds, const uint16_t *rows, int64_t stride, int row0, int T, Swz swz) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = 4 * wave + (lane >> 4), have = min(kTileKeys, T - row0);
+  const __amdgpu_buffer_rsrc_t rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(rows + (int64_t)row0 * stride), (short)0,
+                                        have > 0 ? (int)((have - 1) * stride * 2 + kHeadDim * 2) : 0, 0x00020000);
+#pragma unroll
+  for (int u = 0; u < kTileKeys / 16; ++u) {
+    const int r = row + 16 * u;
+    // (a row past the prompt: past the descriptor whatever the stride)
+    const uint32_t off = r < have ? (uint32_t)r * (uint32_t)(stride * 2) + 16u * (uint32_t)((lane & 15) ^ swz(r)) : 0x7ffffff0u;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void *)(lds + (16 * u + 4 * wave) * kRowWords), 16, off, 0, 0, 0);
+  }
+}
+// K: 16 lanes read one word of 16 rows; V: 32 lanes read 32 bytes of four rows twice.
+__device__ inline int swz_k(int r) { return r & 15; }
+__device__ inline int swz_v(int r) { return 4 * (r & 3); }
+
+// V^T operand of channels [32 c, 32 c + 32) and keys 16 kh .. + 15 of a 32-key
+// subtile: lane l holds channel 32 c + l % 32, keys 16 kh + 4 (l / 32) + {0..3, 8..11}.
+__device__ inline uint32_t v_offset() {
+  const int lane = threadIdx.x & 63, i = lane & 15;
+  return (uint32_t)((4 * (lane >> 5) + (i >> 2)) * 256 + 64 * (i >> 2) + 32 * ((lane >> 4) & 1) + 8 * (i & 3));
+}
+__device__ inline u4_t read_v(const u4_t *tile, uint32_t off, int c, int kh) {
+  const char *p = reinterpret_cast<const char *>(tile) + (off ^ (64u * c)) + 256 * 16 * kh;
+  typedef __attribute__((address_space(3))) s4_t *lds_s4;
+  const s4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(p));
+  const s4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(p + 256 * 8));
+  const uint2 x = __builtin_bit_cast(uint2, a), y = __builtin_bit_cast(uint2, b);
+  return u4_t{x.x, x.y, y.x, y.y};
+}
+
+__device__ inline float tanh_of(float y) {
+  const float e = __builtin_amdgcn_exp2f(y * (2.0f * kLog2e));
+  return fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + e), 1.0f);
+}
+
+// How a tile's accumulators become scores in log2 units less the query's maximum:
+//   RAW:  x = fma(d, scale, fma(slope, row, base))     (cap: of tanh(d scale) instead of d, times cap)
+// with row the constant part of the key's index; an edge tile's accumulators
+// hold final scores (scale 1, slope 0, no cap).
+struct Coef {
+  float scale, slope, base;
+};
+__host__ __device__ constexpr float row_const(int r) { return (float)(8 * (r >> 2) + (r & 3)); }
+
+template <bool CAP, bool BIAS>
+__device__ inline float term(float d, int r, const Coef &c, float cap) {
+  float a = c.base;
+  if constexpr (BIAS) a = fmaf(c.slope, row_const(r), a);
+  if constexpr (CAP) return fmaf(tanh_of(d * c.scale), cap, a);
+  return fmaf(d, c.scale, a);
+}
+
+__device__ inline uint32_t pack2(float a, float b) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  const h2 v = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// One half step: the logits `next` = key x query, the value product out += vt x w
+// and, between their MFMAs, the weights `p` of the tile `cur`, whose sum is
+// returned.  ahead(i) issues LDS reads after the i-th pair of MFMAs.
+template <bool CAP, bool BIAS, class Ahead>
+__device__ inline float stage(f16_t &next, const u4_t (&key)[8], const u4_t (&query)[8], f16_t (&out)[4],
+                              u4_t (&vt)[4][2], const u4_t (&w)[2], const f16_t &cur, const Coef &c, float cap, u4_t (&p)[2],
+                              Ahead ahead) {
+  f16_t d = splat(0.0f);
+  float ts[2] = {0.0f, 0.0f};
+  float x0 = term<CAP, BIAS>(cur[0], 0, c, cap), x1 = term<CAP, BIAS>(cur[1], 1, c, cap);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    d = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(key[i]), as_h8(query[i]), d, 0, 0, 0);
+    out[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vt[i & 3][i >> 2]), as_h8(w[i >> 2]), out[i & 3], 0, 0, 0);
+    ahead(i);
+    const float p0 = __builtin_amdgcn_exp2f(x0), p1 = __builtin_amdgcn_exp2f(x1);
+    if (i < 7) {
+      x0 = term<CAP, BIAS>(cur[2 * i + 2], 2 * i + 2, c, cap);
+      x1 = term<CAP, BIAS>(cur[2 * i + 3], 2 * i + 3, c, cap);
+    }
+    ts[0] += p0;
+    ts[1] += p1;
+    p[i >> 2][i & 3] = pack2(p0, p1);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  next = d;
+  return ts[0] + ts[1];
+}
+
+__device__ inline int wave_min_int(int v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ inline int wave_max_int(int v) { return -wave_min_int(-v); }
+
+// A query's interval, clamped to the prompt; empty: (0, 0).
+__device__ inline void query_span(const int32_t *begin, const int32_t *end, int64_t at, int i, int T, int &lo, int &hi) {
+  lo = begin ? max(begin[at], 0) : 0;
+  hi = end ? min(end[at], T) : i + 1;
+  if (lo >= hi) lo = hi = 0;
+}
+
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void prompt_attention_kernel(PromptArgs A) {
+  constexpr int TR = kTileKeys;
+  __shared__ u4_t s_k[2][TR * kRowWords];
+  __shared__ u4_t s_v[3][TR * kRowWords];
+  __shared__ int s_span[4][2];
+  const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int G = A.q_heads / A.kv_heads, T = A.T;
+  int hk, idx;
+  if (!block_unit(A.units, A.nblk * G, A.run, hk, idx)) return;
+  const int b = hk / A.kv_heads, kvh = hk % A.kv_heads, head = kvh * G + idx % G;
+  const int i_wave = (A.nblk - 1 - idx / G) * kBlockRows + kWaveRows * wave;
+  const uint16_t *kb = A.k + b * A.ks[0] + kvh * A.ks[1], *vb = A.v + b * A.vs[0] + kvh * A.vs[1];
+  const uint16_t *qb = A.q + b * A.qs[0] + head * A.qs[1];
+
+  // The queries, and their intervals (queries past the prompt repeat the last one).
+  u4_t bq[2][8];
+  int lo[2], hi[2], i_own[2], full_lo[2], full_hi[2];
+  int any_lo = T, any_hi = 0;
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const int i = min(i_wave + 32 * cb + n, T - 1);
+    i_own[cb] = i;
+    const uint16_t *r = qb + (int64_t)i * A.qs[2] + 8 * half;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) bq[cb][c] = *reinterpret_cast<const u4_t *>(r + 16 * c);
+    query_span(A.begin, A.end, (int64_t)b * T + i, i, T, lo[cb], hi[cb]);
+    full_lo[cb] = wave_max_int(lo[cb]);
+    full_hi[cb] = wave_min_int(hi[cb]);
+    any_lo = min(any_lo, wave_min_int(hi[cb] ? lo[cb] : T));
+    any_hi = max(any_hi, wave_max_int(hi[cb]));
+  }
+  if (lane == 0) {
+    s_span[wave][0] = any_lo;
+    s_span[wave][1] = any_hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    any_lo = min(any_lo, s_span[w][0]);
+    any_hi = max(any_hi, s_span[w][1]);
+  }
+  any_lo = __builtin_amdgcn_readfirstlane(any_lo);
+  any_hi = __builtin_amdgcn_readfirstlane(any_hi);
+  const int t_first = any_lo / TR, t_end = max(t_first, (any_hi + TR - 1) / TR);
+
+  const float slope = BIAS ? A.slopes[head] * kLog2e : 0.0f;
+  float m[2] = {-kInf, -kInf}, l[2] = {0.0f, 0.0f};
+  f16_t o[2][4];
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[cb][c] = splat(0.0f);
+
+  if (t_first < t_end) {
+    const int i_lo[2] = {min(i_wave, T - 1), min(i_wave + 32, T - 1)};
+    const int i_hi[2] = {min(i_wave + 31, T - 1), min(i_wave + 63, T - 1)};
+    // whether every query of tile cb sees keys j0 .. j0 + 31, on one side of it where the bias needs that
+    auto full = [&](int cb, int j0) {
+      bool f = j0 >= full_lo[cb] && j0 + 32 <= full_hi[cb];
+      if constexpr (BIAS) f = f && (j0 + 31 <= i_lo[cb] || j0 > i_hi[cb]);
+      return f;
+    };
+    auto coef = [&](int cb, int j0) {
+      Coef c;
+      c.scale = A.scale;
+      c.slope = 0.0f;
+      c.base = -m[cb];
+      if constexpr (BIAS) {
+        c.slope = j0 > i_hi[cb] ? -slope : slope;
+        c.base = fmaf(c.slope, (float)(j0 + 4 * half - i_own[cb]), c.base);
+      }
+      return c;
+    };
+    // final scores of a tile of which not every query sees every key
+    auto edge = [&](f16_t &d, int cb, int j0) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = j0 + tile_row(r);
+        float s = CAP ? tanh_of(d[r] * A.scale) * A.cap : d[r] * A.scale;
+        if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own[cb] - j), s);
+        d[r] = j >= lo[cb] && j < hi[cb] ? s : -kInf;
+      }
+    };
+    // Where a tile's weights sum past kRaise (or are NaN: the maximum starts at
+    // -inf) in any lane: raise the maxima, rescale, and weigh the tile again.
+    // The two lanes of a query keep one maximum.
+    auto settle = [&](const f16_t &d, bool is_full, int cb, int j0, float ts, u4_t (&p)[2]) {
+      if (__ballot(!(ts <= kRaise))) {
+        Coef c = coef(cb, j0);
+        c.base += m[cb] == -kInf ? -kInf : m[cb];
+        if (m[cb] == -kInf) c.base = BIAS && is_full ? c.slope * (float)(j0 + 4 * half - i_own[cb]) : 0.0f;
+        if (!is_full) c.base = 0.0f;
+        float s[16], mx = -kInf;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = is_full ? term<CAP, BIAS>(d[r], r, c, A.cap) : d[r];
+          mx = fmaxf(mx, s[r]);
+        }
+        mx = fmaxf(m[cb], fmaxf(mx, __shfl_xor(mx, 32, 64)));
+        const float ref = mx == -kInf ? 0.0f : mx;
+        const float f = m[cb] == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m[cb] - ref);
+        m[cb] = mx;
+        l[cb] *= f;
+#pragma unroll
+        for (int c4 = 0; c4 < 4; ++c4)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[cb][c4][r] *= f;
+        ts = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(s[r] - ref);
+          ts += s[r];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = pack2(s[2 * i], s[2 * i + 1]);
+      }
+      l[cb] += ts;
+    };
+
+    const uint32_t off = tile_offset(), voff = v_offset();
+    auto load_tile = [&](int t) {
+      stage_rows(s_k[(t - t_first) & 1], kb, A.ks[2], t * TR, T, swz_k);
+      stage_rows(s_v[(t - t_first) % 3], vb, A.vs[2], t * TR, T, swz_v);
+    };
+    load_tile(t_first);
+    if (t_first + 1 < t_end) load_tile(t_first + 1);
+    wait_loads();
+    __syncthreads();
+
+    // Before the first subtile: weights and value operands of zero, and a second
+    // tile that sees nothing (edge form), with its first key.
+    u4_t kf[8], vf[4][2], p0[2], p1[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) vf[i & 3][i >> 2] = u4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p0[i] = p1[i] = u4_t{0, 0, 0, 0};
+    read_tile(s_k[0], off, 0, kf);
+    // A value of a row that some query does not see must not reach that query as
+    // 0 x NaN: in an edge subtile infinities and NaN are taken out of the value
+    // operand (clean says whether any were there), and the queries that do see
+    // one become NaN in its channel (poison, once the subtile's weights are known).
+    auto odd_halves = [](uint32_t w) { return (((w & 0x7fff7fffu) + 0x04000400u) & 0x80008000u) >> 15; };  // 1 per infinite or NaN half
+    auto clean = [&]() {
+      uint32_t any = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= odd_halves(vf[i & 3][i >> 2][e]);
+      if (!__ballot(any != 0u)) return false;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vf[i & 3][i >> 2][e] &= ~(odd_halves(vf[i & 3][i >> 2][e]) * 0xffffu);
+      return true;
+    };
+    auto poison = [&](int s, const u4_t (&w0)[2], const u4_t (&w1)[2]) {
+      const u4_t *v = s_v[(s >> 1) % 3] + 32 * (s & 1) * kRowWords;
+      auto ones = [](uint32_t w) { return ((w & 0xffffu) ? 0x3c00u : 0u) | ((w >> 16) ? 0x3c000000u : 0u); };
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int cb = 0; cb < 2; ++cb) {
+          f16_t hits = splat(0.0f);
+#pragma unroll
+          for (int kh = 0; kh < 2; ++kh) {
+            u4_t a = read_v(v, voff, c, kh), w = cb ? w1[kh] : w0[kh];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              a[e] = odd_halves(a[e]) * 0x3c00u;
+              w[e] = ones(w[e]);
+            }
+            hits = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(a), as_h8(w), hits, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[cb][c][r] += hits[r] > 0.0f ? __builtin_nanf("") : 0.0f;
+        }
+    };
+    f16_t d0, d1 = splat(-kInf);
+    bool full1 = false, bad = false;
+    int j1 = t_first * TR;
+    const int n_sub = 2 * (t_end - t_first);
+    for (int s = 0; s < n_sub; ++s) {
+      const int t = s >> 1, j0 = t_first * TR + 32 * s;
+      // stage 1: logits of the first query tile, value product of its tile
+      // before, weights of the second query tile before
+      float ts;
+      auto none = [](int) {};
+      if (CAP && !full1)
+        ts = stage<false, false>(d0, kf, bq[0], o[0], vf, p0, d1, Coef{1.0f, 0.0f, -m[1]}, A.cap, p1, none);
+      else
+        ts = stage<CAP, BIAS>(d0, kf, bq[0], o[0], vf, p0, d1, full1 ? coef(1, j1) : Coef{1.0f, 0.0f, -m[1]}, A.cap, p1, none);
+      settle(d1, full1, 1, j1, ts, p1);
+      if (bad) poison(s - 1, p0, p1);
+      const bool full0 = full(0, j0);
+      if (!full0) edge(d0, 0, j0);
+      // the last subtile of a tile: the next tile is complete, and every wave is
+      // done with this tile's keys and the value rows of the one before
+      if (s & 1) {
+        wait_loads();
+        __syncthreads();
+      }
+      // stage 2: the same for the second query tile, the weights of the first;
+      // the next subtile's keys and this one's value rows are read on the way
+      const u4_t *kn = s_k[((s + 1) >> 1) & 1], *vn = s_v[t % 3] + 32 * (s & 1) * kRowWords;
+      const int kr = 32 * ((s + 1) & 1);
+      auto ahead = [&](int i) {
+        kf[i] = read_word(kn, off, kr, i);
+        vf[i & 3][i >> 2] = read_v(vn, voff, i & 3, i >> 2);
+      };
+      if (CAP && !full0)
+        ts = stage<false, false>(d1, kf, bq[1], o[1], vf, p1, d0, Coef{1.0f, 0.0f, -m[0]}, A.cap, p0, ahead);
+      else
+        ts = stage<CAP, BIAS>(d1, kf, bq[1], o[1], vf, p1, d0, full0 ? coef(0, j0) : Coef{1.0f, 0.0f, -m[0]}, A.cap, p0, ahead);
+      if ((s & 1) && t_first + t + 2 < t_end) load_tile(t_first + t + 2);
+      settle(d0, full0, 0, j0, ts, p0);
+      full1 = full(1, j0);
+      j1 = j0;
+      if (!full1) edge(d1, 1, j0);
+      bad = !(full0 && full1) && clean();
+    }
+    // the weights of the last second query tile, and both last value products
+    {
+      const Coef c = full1 ? coef(1, j1) : Coef{1.0f, 0.0f, -m[1]};
+      float ts = 0.0f, x[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        x[r] = __builtin_amdgcn_exp2f(full1 ? term<CAP, BIAS>(d1[r], r, c, A.cap) : d1[r] + c.base);
+        ts += x[r];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p1[i >> 2][i & 3] = pack2(x[2 * i], x[2 * i + 1]);
+      settle(d1, full1, 1, j1, ts, p1);
+      if (bad) poison(n_sub - 1, p0, p1);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      o[0][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p0[i >> 2]), o[0][i & 3], 0, 0, 0);
+      o[1][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p1[i >> 2]), o[1][i & 3], 0, 0, 0);
+    }
+  }
+
+  // out = O / l, through LDS so that whole rows are stored
+  wait_loads();
+  __syncthreads();
+  u4_t *rows = wave < 2 ? s_k[wave] : s_v[wave - 2];  // 16 KiB each
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const float sum = l[cb] + __shfl_xor(l[cb], 32, 64);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int i = i_wave + 32 * cb + n;
+    if (A.lse && half == 0 && i < T)
+      A.lse[((int64_t)b * A.q_heads + head) * T + i] = sum == 0.0f ? -kInf : (m[cb] + __builtin_amdgcn_logf(sum)) * kLn2;
+    uint2 *row = reinterpret_cast<uint2 *>(rows) + (32 * cb + n) * (2 * kRowWords);
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const int w = 4 * c + a;  // 16-byte word: channels 32 c + 8 a ..
+        row[2 * (w ^ (n & 15)) + half] = make_uint2(pack2(o[cb][c][4 * a] * inv, o[cb][c][4 * a + 1] * inv),
+                                                   pack2(o[cb][c][4 * a + 2] * inv, o[cb][c][4 * a + 3] * inv));
+      }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+  uint16_t *ob = A.out + b * A.os[0] + head * A.os[1];
+#pragma unroll
+  for (int u = 0; u < 16; ++u) {
+    const int r = 4 * u + (lane >> 4), i = i_wave + r;
+    const u4_t w = rows[r * kRowWords + ((lane & 15) ^ (r & 15))];
+    if (i < T) *reinterpret_cast<u4_t *>(ob + (int64_t)i * A.os[2] + 8 * (lane & 15)) = w;
+  }
+}
+
+// H2O importance under the rules: a wave holds 64 keys of one KV head and streams
+// the queries of every head of the group past them (queries along the tile's
+// columns, so a lane holds one query per tile, whose log-sum-exp and interval are
+// scalars), as prefill_colsum_kernel does for the causal case.  WS waves of the
+// block take the same keys and share out the 32-query subtiles.
+struct SumArgs {
+  const uint16_t *q, *k;
+  int64_t qs[3], ks[3];
+  const float *lse, *slopes;
+  const int32_t *begin, *end;
+  const int4 *spans;  // of every 32 queries, or NULL (causal)
+  float *scores;
+  int q_heads, kv_heads, units, nblk, run, T;
+  float scale, cap;
+};
+
+// Interval extremes of 32 queries: smallest begin and largest end over those that
+// see something, largest begin and smallest end over all (the latter 0 if one
+// sees nothing).
+__global__ __launch_bounds__(64) void query_spans_kernel(const int32_t *begin, const int32_t *end, int T, int nsub, int4 *spans) {
+  const int b = blockIdx.y, i = blockIdx.x * 64 + threadIdx.x;
+  int lo = 0, hi = 0;
+  if (i < T) query_span(begin, end, (int64_t)b * T + i, i, T, lo, hi);
+  int a = hi ? lo : T, z = hi, x = lo, y = hi;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    a = min(a, __shfl_xor(a, o, 64));
+    z = max(z, __shfl_xor(z, o, 64));
+    x = max(x, __shfl_xor(x, o, 64));
+    y = min(y, __shfl_xor(y, o, 64));
+  }
+  if ((threadIdx.x & 31) == 0 && i / 32 < nsub) spans[(int64_t)b * nsub + i / 32] = make_int4(a, z, x, y);
+}
+
+__device__ inline int4 causal_span(int i0, int T) {
+  return i0 >= T ? make_int4(T, 0, 0, 0) : make_int4(0, min(i0 + 32, T), 0, i0 + 31 < T ? i0 + 1 : 0);
+}
+
+template <int WS>
+constexpr int sum_rows() { return WS == 4 ? 128 : 64; }
+
+template <int WS, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
+void prompt_colsum_kernel(SumArgs A) {
+  constexpr int TR = sum_rows<WS>(), SUBS = TR / 32 / WS, kKeys = kWaveRows * 4 / WS;
+  __shared__ u4_t s_rows[2][TR * kRowWords];
+  __shared__ float s_lse[2][TR];
+  __shared__ int2 s_span[2][TR];
+  __shared__ int4 s_sub[2][TR / 32];
+  __shared__ float s_sum[4][kWaveRows];
+  __shared__ int s_range[4][2];
+  const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5, tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wc = wave / WS, ws = wave % WS;
+  const int G = A.q_heads / A.kv_heads, T = A.T, nsub = (T + 31) / 32;
+  int hk, idx;
+  if (!block_unit(A.units, A.nblk, A.run, hk, idx)) return;
+  const int b = hk / A.kv_heads, kvh = hk % A.kv_heads;
+  const int j_base = idx * kKeys, j_wave = j_base + kWaveRows * wc;
+  const uint16_t *qb = A.q + b * A.qs[0] + (int64_t)kvh * G * A.qs[1], *kb = A.k + b * A.ks[0] + kvh * A.ks[1];
+  auto sub_span = [&](int sub) {
+    if (sub >= nsub) return make_int4(T, 0, 0, 0);
+    return A.spans ? A.spans[(int64_t)b * nsub + sub] : causal_span(32 * sub, T);
+  };
+  // the query tiles between the first and the last that see any of the block's keys
+  int first = nsub, last = -1;
+  for (int s = tid; s < nsub; s += kThreads) {
+    const int4 v = sub_span(s);
+    if (v.x < j_base + kKeys && v.y > j_base) {
+      first = min(first, s);
+      last = s;
+    }
+  }
+  first = min(wave_min_int(first), wave_min_int(__shfl_xor(first, 32, 64)));
+  last = max(wave_max_int(last), wave_max_int(__shfl_xor(last, 32, 64)));
+  if (lane == 0) {
+    s_range[wave][0] = first;
+    s_range[wave][1] = last;
+  }
+  u4_t ak[2][8];
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb) {
+    const uint16_t *r = kb + (int64_t)min(j_wave + 32 * cb + n, T - 1) * A.ks[2] + 8 * half;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) ak[cb][c] = *reinterpret_cast<const u4_t *>(r + 16 * c);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    first = min(first, s_range[w][0]);
+    last = max(last, s_range[w][1]);
+  }
+  first = __builtin_amdgcn_readfirstlane(first);
+  last = __builtin_amdgcn_readfirstlane(last);
+  const int t_first = 32 * first / TR, t_end = last < first ? t_first : 32 * last / TR + 1;
+
+  f16_t cs[2] = {splat(0.0f), splat(0.0f)};
+  float r_lse = 0.0f;
+  int2 r_span = make_int2(0, 0);
+  int4 r_sub = make_int4(0, 0, 0, 0);
+  auto load = [&](int buf, int g, int t) {
+    const uint16_t *rows = qb + g * A.qs[1];
+#pragma unroll
+    for (int u = 0; u < TR / 64; ++u)
+      stage_rows(s_rows[buf] + 64 * u * kRowWords, rows, A.qs[2], t * TR + 64 * u, T, swz_k);
+    if (tid < TR) {
+      const int i = t * TR + tid, ic = min(i, T - 1);
+      r_lse = A.lse[((int64_t)b * A.q_heads + kvh * G + g) * T + ic] * kLog2e;
+      int lo, hi;
+      query_span(A.begin, A.end, (int64_t)b * T + ic, ic, T, lo, hi);
+      r_span = i < T ? make_int2(lo, hi) : make_int2(0, 0);
+    }
+    if (tid < TR / 32) r_sub = sub_span(t * (TR / 32) + tid);
+  };
+  auto commit = [&](int buf) {
+    if (tid < TR) {
+      s_lse[buf][tid] = r_lse;
+      s_span[buf][tid] = r_span;
+    }
+    if (tid < TR / 32) s_sub[buf][tid] = r_sub;
+    wait_loads();
+    __syncthreads();
+  };
+  const uint32_t off = tile_offset();
+  if (t_first < t_end) {
+    load(0, 0, t_first);
+    commit(0);
+    int buf = 0;
+    for (int g = 0; g < G; ++g) {
+      const float slope = BIAS ? A.slopes[kvh * G + g] * kLog2e : 0.0f;
+      for (int t = t_first; t < t_end; ++t) {
+        const bool wrap = t + 1 == t_end;
+        load(buf ^ 1, wrap ? min(g + 1, G - 1) : g, wrap ? t_first : t + 1);
+        const u4_t *rows = s_rows[buf];
+#pragma unroll
+        for (int s = 0; s < SUBS; ++s) {
+          const int sub = ws * SUBS + s, i0 = t * TR + 32 * sub;
+          const int4 sp = s_sub[buf][sub];
+          const int any_lo = __builtin_amdgcn_readfirstlane(sp.x), any_hi = __builtin_amdgcn_readfirstlane(sp.y);
+          const int full_lo = __builtin_amdgcn_readfirstlane(sp.z), full_hi = __builtin_amdgcn_readfirstlane(sp.w);
+          if (any_lo >= j_wave + kWaveRows || any_hi <= j_wave) continue;  // wave-uniform
+          u4_t bq[8];
+          read_tile(rows, off, 32 * sub, bq);
+          const float lse2 = s_lse[buf][32 * sub + n];
+          const int2 span = s_span[buf][32 * sub + n];
+          const int i = min(i0 + n, T - 1);
+#pragma unroll
+          for (int cb = 0; cb < 2; ++cb) {
+            const int j0 = j_wave + 32 * cb;
+            const f16_t d = logits(ak[cb], bq);
+            bool full = j0 >= full_lo && j0 + 32 <= full_hi;
+            if constexpr (BIAS) full = full && (j0 + 31 <= i0 || j0 > i0 + 31);
+            if (full) {
+              Coef c = {A.scale, 0.0f, -lse2};
+              if constexpr (BIAS) {
+                c.slope = j0 > i0 ? -slope : slope;
+                c.base = fmaf(c.slope, (float)(j0 + 4 * half - i), c.base);
+              }
+#pragma unroll
+              for (int r = 0; r < 16; ++r) cs[cb][r] += __builtin_amdgcn_exp2f(term<CAP, BIAS>(d[r], r, c, A.cap));
+            } else {
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const int j = j0 + tile_row(r);
+                float x = CAP ? tanh_of(d[r] * A.scale) * A.cap : d[r] * A.scale;
+                if constexpr (BIAS) x = fmaf(-slope, (float)abs(i - j), x);
+                const float p = __builtin_amdgcn_exp2f(x - lse2);
+                cs[cb][r] += j >= span.x && j < span.y ? p : 0.0f;
+              }
+            }
+          }
+        }
+        buf ^= 1;
+        commit(buf);
+      }
+    }
+  }
+  // over the tile's 32 query columns, then over the WS waves
+#pragma unroll
+  for (int cb = 0; cb < 2; ++cb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float v = cs[cb][r];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+      if (n == 0) s_sum[wave][32 * cb + tile_row(r)] = v;
+    }
+  __syncthreads();
+  if (ws != 0) return;
+  float v = s_sum[wave][lane];
+#pragma unroll
+  for (int o = 1; o < WS; ++o) v += s_sum[wave + o][lane];
+  const int kj = j_wave + lane;
+  if (kj < T) A.scores[(int64_t)hk * T + kj] = v;
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+
+// The rows of one tensor: 16-byte aligned, strides multiples of 8, and a tile's
+// byte offsets (64 rows) within 31 bits.
+int check_rows(const char *who, const char *name, const void *p, const int64_t s[3]) {
+  if (!p) return set_error(MIKV_ERR_INVALID_ARG, "%s: %s is NULL", who, name);
+  if ((uintptr_t)p % 16 || s[0] % 8 || s[1] % 8 || s[2] % 8)
+    return set_error(MIKV_ERR_INVALID_ARG, "%s: %s: rows must be 16-byte aligned, strides multiples of 8", who, name);
+  if (s[0] < 0 || s[1] < 0 || s[2] < 0) return set_error(MIKV_ERR_INVALID_ARG, "%s: %s: negative stride", who, name);
+  if (s[2] > (int64_t)1 << 22) return set_error(MIKV_ERR_UNSUPPORTED, "%s: %s: token stride over 2^22", who, name);
+  return MIKV_OK;
+}
+
+int check_prompt(const char *who, const mikv_prompt *p, const mikv_score_rules *r) {
+  if (!p) return set_error(MIKV_ERR_INVALID_ARG, "%s: prompt is NULL", who);
+  if (p->batch < 1 || p->q_heads < 1 || p->kv_heads < 1 || p->tokens < 1 || p->q_heads % p->kv_heads)
+    return set_error(MIKV_ERR_INVALID_ARG, "%s: bad sizes", who);
+  const int G = p->q_heads / p->kv_heads;
+  if (G != 1 && G != 2 && G != 4 && G != 8)
+    return set_error(MIKV_ERR_UNSUPPORTED, "%s: query heads per KV head must be 1, 2, 4 or 8", who);
+  if (p->head_dim != kHeadDim) return set_error(MIKV_ERR_UNSUPPORTED, "%s: head_dim must be %d", who, kHeadDim);
+  if (!(p->scale > 0.0f) || p->scale == kInf) return set_error(MIKV_ERR_INVALID_ARG, "%s: scale must be > 0", who);
+  if (p->tokens > 1 << 30) return set_error(MIKV_ERR_UNSUPPORTED, "%s: over 2^30 tokens", who);
+  // blocks of 64 rows at most, rounded up to whole groups and runs
+  if ((int64_t)(p->batch * (int64_t)p->q_heads + 8 * G) * ((p->tokens + 63) / 64 + 32) > (int64_t)1 << 22 << 9)
+    return set_error(MIKV_ERR_UNSUPPORTED, "%s: too many blocks", who);
+  if (int e = check_rows(who, "q", p->q, p->q_stride)) return e;
+  if (int e = check_rows(who, "k", p->k, p->k_stride)) return e;
+  if (r) {
+    if (!(r->cap >= 0.0f) || r->cap == kInf) return set_error(MIKV_ERR_INVALID_ARG, "%s: cap must be >= 0", who);
+    if (((uintptr_t)r->slopes | (uintptr_t)r->begin | (uintptr_t)r->end) % 4)
+      return set_error(MIKV_ERR_INVALID_ARG, "%s: misaligned rules", who);
+  }
+  return MIKV_OK;
+}
+
+// log2 units: s log2(e) = scale' d, or cap' tanh(scale' d)
+void score_scales(float scale, float cap, float &s, float &c) {
+  c = cap * kLog2e;
+  s = cap > 0.0f ? scale / cap : scale * kLog2e;
+}
+
+unsigned grid_blocks(int units, int per_unit, int run) {
+  return (unsigned)(8 * ((units + 7) / 8) * (((int64_t)per_unit + run - 1) / run * run));
+}
+
+template <class T>
+void copy3(T d[3], const T s[3]) { d[0] = s[0], d[1] = s[1], d[2] = s[2]; }
+
+template <int WS>
+void launch_colsum(const SumArgs &A, dim3 grid, hipStream_t st) {
+  const bool cap = A.cap > 0.0f, bias = A.slopes != nullptr;
+  auto kernel = cap ? (bias ? prompt_colsum_kernel<WS, true, true> : prompt_colsum_kernel<WS, true, false>)
+                    : (bias ? prompt_colsum_kernel<WS, false, true> : prompt_colsum_kernel<WS, false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, A);
+}
+
+}  // namespace
+
+}  // namespace mikv
+
+using namespace mikv;
+
+extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rules *rules, uint16_t *out,
+                                     const int64_t out_stride[3], float *lse, void *stream) {
+  const char *who = "mikv_prompt_attention";
+  if (int e = check_prompt(who, p, rules)) return e;
+  if (int e = check_rows(who, "v", p->v, p->v_stride)) return e;
+  if (!out_stride) return set_error(MIKV_ERR_INVALID_ARG, "%s: out_stride is NULL", who);
+  if (int e = check_rows(who, "out", out, out_stride)) return e;
+  if ((uintptr_t)lse % 4) return set_error(MIKV_ERR_INVALID_ARG, "%s: misaligned lse", who);
+  PromptArgs A{};
+  A.q = p->q, A.k = p->k, A.v = p->v, A.out = out, A.lse = lse;
+  copy3(A.qs, p->q_stride), copy3(A.ks, p->k_stride), copy3(A.vs, p->v_stride), copy3(A.os, out_stride);
+  if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end;
+  A.q_heads = p->q_heads, A.kv_heads = p->kv_heads, A.T = p->tokens;
+  A.units = p->batch * p->kv_heads;
+  A.nblk = (p->tokens + kBlockRows - 1) / kBlockRows;
+  const int per_unit = A.nblk * (p->q_heads / p->kv_heads);
+  A.run = std::min((int64_t)A.units * per_unit >= 4096 ? 32 : 4, per_unit);
+  score_scales(p->scale, rules ? rules->cap : 0.0f, A.scale, A.cap);
+  const dim3 grid(grid_blocks(A.units, per_unit, A.run));
+  const bool cap = A.cap > 0.0f, bias = A.slopes != nullptr;
+  auto kernel = cap ? (bias ? prompt_attention_kernel<true, true> : prompt_attention_kernel<true, false>)
+                    : (bias ? prompt_attention_kernel<false, true> : prompt_attention_kernel<false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, A);
+  return check_launch(who);
+}
+
+extern "C" size_t mikv_prompt_importance_workspace_size(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t tokens) {
+  if (batch < 1 || q_heads < 1 || kv_heads < 1 || tokens < 1) return 0;
+  return (size_t)batch * (((size_t)tokens + 31) / 32) * sizeof(int4);
+}
+
+extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rules *rules, const float *lse, float *scores,
+                                      void *ws, size_t ws_bytes, void *stream) {
+  const char *who = "mikv_prompt_importance";
+  if (int e = check_prompt(who, p, rules)) return e;
+  if (!lse || !scores || ((uintptr_t)lse | (uintptr_t)scores) % 4)
+    return set_error(MIKV_ERR_INVALID_ARG, "%s: NULL or misaligned lse or scores", who);
+  if (!ws || ws_bytes < mikv_prompt_importance_workspace_size(p->batch, p->q_heads, p->kv_heads, p->tokens))
+    return set_error(MIKV_ERR_CAPACITY, "%s: workspace too small", who);
+  if ((uintptr_t)ws % 16) return set_error(MIKV_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+  hipStream_t st = (hipStream_t)stream;
+  SumArgs A{};
+  A.q = p->q, A.k = p->k, A.lse = lse, A.scores = scores;
+  copy3(A.qs, p->q_stride), copy3(A.ks, p->k_stride);
+  if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end;
+  A.q_heads = p->q_heads, A.kv_heads = p->kv_heads, A.T = p->tokens;
+  A.units = p->batch * p->kv_heads;
+  score_scales(p->scale, rules ? rules->cap : 0.0f, A.scale, A.cap);
+  if (A.begin || A.end) {
+    const int nsub = (p->tokens + 31) / 32;
+    A.spans = (const int4 *)ws;
+    for (int b = 0; b < p->batch; b += 65535)
+      hipLaunchKernelGGL(query_spans_kernel, dim3((p->tokens + 63) / 64, std::min(65535, p->batch - b)), dim3(64), 0, st,
+                         A.begin ? A.begin + (int64_t)b * p->tokens : nullptr, A.end ? A.end + (int64_t)b * p->tokens : nullptr,
+                         p->tokens, nsub, (int4 *)ws + (int64_t)b * nsub);
+  }
+  // waves on the same keys, by the blocks of 256 keys: as for the causal scores
+  // (plan_pass), fewer keys per block only while the grid leaves CUs idle
+  const int64_t n1 = (int64_t)A.units * ((p->tokens + 255) / 256);
+  const int ws_ = n1 >= 768 ? 1 : n1 >= 192 ? 2 : 4, keys = kWaveRows * 4 / ws_;
+  A.nblk = (p->tokens + keys - 1) / keys;
+  A.run = std::min(n1 >= 4096 ? 32 : 4, A.nblk);
+  const dim3 grid(grid_blocks(A.units, A.nblk, A.run));
+  if (ws_ == 1)
+    launch_colsum<1>(A, grid, st);
+  else if (ws_ == 2)
+    launch_colsum<2>(A, grid, st);
+  else
+    launch_colsum<4>(A, grid, st);
+  return check_launch(who);
+}

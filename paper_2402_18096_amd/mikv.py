@@ -1,4 +1,4 @@
-"""ctypes binding of libmikv.so (C ABI in include/mikv.h).
+"""ctypes binding of libmikv.so (C ABI in include/mikv.h and include/mikv_layer.h).
 
 Argument marshalling only: every function below forwards torch tensors'
 device pointers to the C entry point of the same name, on torch's current
@@ -16,7 +16,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from ctypes import c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 from typing import Optional
 
 import torch
@@ -89,6 +89,46 @@ _SIGS["mikv_set_resident_bytes"] = (c_int32, [c_size_t])
 EXPORTS = tuple(_SIGS)
 
 
+class RotaryScheme(ctypes.Structure):
+    """Mirror of ``struct mikv_rotary_scheme``."""
+    _fields_ = [("rot_dim", c_int32), ("scaling", c_int32), ("base", c_double), ("factor", c_double),
+                ("original_length", c_double), ("low", c_double), ("high", c_double)]
+
+
+class Heads(ctypes.Structure):
+    """Mirror of ``struct mikv_heads``."""
+    _fields_ = [("x", c_void_p), ("y", c_void_p), ("x_stride", c_int64 * 3), ("y_stride", c_int64 * 3),
+                ("heads", c_int32), ("rotate", c_int32)]
+
+
+class RulesDesc(ctypes.Structure):
+    """Mirror of ``struct mikv_score_rules``."""
+    _fields_ = [("cap", c_float), ("slopes", c_void_p), ("begin", c_void_p), ("end", c_void_p)]
+
+
+class PromptDesc(ctypes.Structure):
+    """Mirror of ``struct mikv_prompt``."""
+    _fields_ = [(n, c_int32) for n in ("batch", "q_heads", "kv_heads", "tokens", "head_dim")] + \
+               [("scale", c_float), ("q", c_void_p), ("k", c_void_p), ("v", c_void_p),
+                ("q_stride", c_int64 * 3), ("k_stride", c_int64 * 3), ("v_stride", c_int64 * 3)]
+
+
+_PR, _PP = ctypes.POINTER(RulesDesc), ctypes.POINTER(PromptDesc)
+
+_LAYER_SIGS = {
+    "mikv_rotary_frequencies": (c_int32, [ctypes.POINTER(RotaryScheme), ctypes.POINTER(ctypes.c_uint64),
+                                          ctypes.POINTER(c_float)]),
+    "mikv_rotary": (c_int32, [ctypes.POINTER(Heads), c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p,
+                              c_int32, c_void_p, c_int32, c_int32, c_float, c_void_p]),
+    "mikv_mask_spans": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
+    "mikv_prompt_attention": (c_int32, [_PP, _PR, c_void_p, ctypes.POINTER(c_int64), c_void_p, c_void_p]),
+    "mikv_prompt_importance_workspace_size": (c_size_t, [c_int32, c_int32, c_int32, c_int32]),
+    "mikv_prompt_importance": (c_int32, [_PP, _PR, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+}
+
+LAYER_EXPORTS = tuple(_LAYER_SIGS)
+
+
 def lib():
     """Load libmikv.so (after torch, so both share torch's HIP runtime)."""
     global _LIB
@@ -96,7 +136,7 @@ def lib():
         if not os.path.exists(LIB_PATH):
             raise MikvError(f"{LIB_PATH} is missing: build it with `python -m paper_2402_18096_amd.build`")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in _SIGS.items():
+        for name, (res, args) in (*_SIGS.items(), *_LAYER_SIGS.items()):
             f = getattr(L, name)
             f.restype, f.argtypes = res, args
         _LIB = L
@@ -426,6 +466,160 @@ def mikv_decode_step_noalloc(cache: MikvCache, length: int, q, k_new, v_new, out
     _check(lib().mikv_decode_step_noalloc(cache.ref(), length, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(balance),
                                           scale, _ptr(out), _ptr(probs_hi), _ptr(probs_lo), k_heavy, window, flags,
                                           ev, _stream()), "mikv_decode_step_noalloc")
+
+
+# -- the layer around the cache -----------------------------------------------------
+
+_TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
+
+
+def _rows(t: torch.Tensor, shape, name: str):
+    """Strides (batch, head, token) of [B, H, T, 128] rows, whose channels have to be contiguous.  A
+    dimension of one element has no stride of its own."""
+    if t.dim() != 4 or t.shape[3] != HEAD_DIM or (shape is not None and t.shape != shape):
+        raise MikvError(f"{name}: expected shape {tuple(shape) if shape else ('B', 'H', 'T', HEAD_DIM)}, "
+                        f"got {tuple(t.shape)}")
+    if not t.is_cuda:
+        raise MikvError(f"{name}: must be a device tensor")
+    st = t.stride()
+    if st[3] != 1:
+        raise MikvError(f"{name}: channels must be contiguous")
+    return [st[i] if t.shape[i] > 1 else 0 for i in range(3)]
+
+
+class MikvRotary:
+    """Frequencies of one rotary scheme on the device, computed once
+    (mikv_rotary_frequencies).  ``scaling``: "none", "linear", "ntk", "bands" or
+    "yarn"; ``low``/``high`` are turns over ``original_length`` (default 1 and 4, for yarn
+    1 and 32); ``magnitude`` replaces the scheme's own factor on rotated channels."""
+
+    def __init__(self, rot_dim: int = HEAD_DIM, base: float = 10000.0, interleaved: bool = False, scaling: str = "none",
+                 factor: float = 1.0, original_length: float = 4096, low: float = 1.0, high: Optional[float] = None,
+                 magnitude: Optional[float] = None, device="cuda"):
+        if scaling not in _SCALINGS:
+            raise MikvError(f"MikvRotary: unknown scaling {scaling!r}")
+        high = (32.0 if scaling == "yarn" else 4.0) if high is None else high
+        freq, m = (ctypes.c_uint64 * (HEAD_DIM // 2))(), c_float()
+        scheme = RotaryScheme(rot_dim, _SCALINGS[scaling], base, factor, original_length, low, high)
+        _check(lib().mikv_rotary_frequencies(ctypes.byref(scheme), freq, ctypes.byref(m)), "mikv_rotary_frequencies")
+        signed = [f - (1 << 64) if f >= 1 << 63 else f for f in freq[:rot_dim // 2]]
+        self.rot_dim, self.interleaved = rot_dim, bool(interleaved)
+        self.magnitude = m.value if magnitude is None else float(magnitude)
+        self.freq = torch.tensor(signed, dtype=torch.int64, device=device)
+
+
+def mikv_rotary(rotary: MikvRotary, xs, ys, positions: Optional[torch.Tensor] = None, pos0: int = 0,
+                rotate=(True, True, False)):
+    """Rotate up to three tensors of the same tokens in one launch: ``xs[i]`` -> ``ys[i]``, each [B, H_i, T, 128]
+    with any strides (channels contiguous), e.g. queries, keys and values as views of a fused projection into
+    contiguous fp16 rows.  Where ``rotate[i]`` is false the rows are converted only.  ``positions`` int32 [B, T], or
+    pos0, pos0 + 1, ... in every sequence."""
+    n = len(xs)
+    if not 1 <= n <= 3 or len(ys) != n or len(rotate) < n:
+        raise MikvError("mikv_rotary: one to three tensors, and as many outputs, expected")
+    B, _, T, _ = xs[0].shape if xs[0].dim() == 4 else (0, 0, 0, 0)
+    arr = (Heads * n)()
+    for i, (x, y) in enumerate(zip(xs, ys)):
+        if x.dim() != 4 or x.shape[0] != B or x.shape[2] != T:
+            raise MikvError("mikv_rotary: [B, H, T, 128] tensors of the same tokens expected")
+        if x.dtype is not xs[0].dtype or y.dtype is not ys[0].dtype or x.dtype not in _TYPES or y.dtype not in _TYPES:
+            raise MikvError("mikv_rotary: one input and one output type of fp16, bf16 and fp32 expected")
+        h = arr[i]
+        h.x, h.y, h.heads, h.rotate = x.data_ptr(), y.data_ptr(), x.shape[1], int(bool(rotate[i]))
+        h.x_stride[:] = _rows(x, None, "x")
+        h.y_stride[:] = _rows(y, x.shape, "y")
+    if positions is not None:
+        _require(positions, torch.int32, (B, T), "positions")
+    _check(lib().mikv_rotary(arr, n, B, T, HEAD_DIM, _TYPES[xs[0].dtype], _TYPES[ys[0].dtype], _ptr(positions), pos0,
+                             _ptr(rotary.freq), rotary.rot_dim, int(rotary.interleaved), rotary.magnitude, _stream()),
+           "mikv_rotary")
+
+
+class ScoreRules:
+    """Score rules of an attention (``struct mikv_score_rules``): tanh ``cap`` (0: none), ``slopes`` fp32 [Hq] of the
+    bias by distance, and the keys that a query sees: ``begin``/``end`` int32 [B, T] of a prompt (mikv_mask_spans), or
+    ``begin`` int32 [B] of a decode step."""
+
+    def __init__(self, cap: float = 0.0, slopes: Optional[torch.Tensor] = None, begin: Optional[torch.Tensor] = None,
+                 end: Optional[torch.Tensor] = None):
+        self.cap, self.slopes, self.begin, self.end = float(cap), slopes, begin, end
+
+    def desc(self, q_heads: int, span_shape) -> RulesDesc:
+        if self.slopes is not None:
+            _require(self.slopes, torch.float32, (q_heads,), "slopes")
+        for name in ("begin", "end"):
+            if getattr(self, name) is not None:
+                _require(getattr(self, name), torch.int32, span_shape, name)
+        return RulesDesc(self.cap, _ptr(self.slopes), _ptr(self.begin), _ptr(self.end))
+
+
+def mikv_mask_spans(begin: torch.Tensor, end: torch.Tensor, documents: Optional[torch.Tensor] = None,
+                    prefix: Optional[torch.Tensor] = None, window: int = 0):
+    """The keys [begin, end) that each query of a prompt sees, int32 [B, T]: those of its document (a run of equal
+    ``documents`` int32 [B, T]; negative: padding) that are no later than it or among the ``prefix`` int32 [B] first
+    positions, and, with ``window`` > 0, among the last ``window`` up to it."""
+    if begin.dim() != 2:
+        raise MikvError("mikv_mask_spans: begin [B, T] expected")
+    _require(begin, torch.int32, name="begin")
+    _require(end, torch.int32, begin.shape, "end")
+    B, T = begin.shape
+    if documents is not None:
+        _require(documents, torch.int32, (B, T), "documents")
+    if prefix is not None:
+        _require(prefix, torch.int32, (B,), "prefix")
+    _check(lib().mikv_mask_spans(_ptr(documents), _ptr(prefix), B, T, window, _ptr(begin), _ptr(end), _stream()),
+           "mikv_mask_spans")
+
+
+def _prompt(q, k, v, scale):
+    if q.dim() != 4 or k.dim() != 4:
+        raise MikvError("q [B, Hq, T, 128] and k [B, Hkv, T, 128] expected")
+    B, Hq, T, D = q.shape
+    p = PromptDesc(B, Hq, k.shape[1], T, D, 1.0 / math.sqrt(HEAD_DIM) if scale is None else scale)
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if t is None:
+            continue
+        _require(t, torch.float16, name=name)
+        setattr(p, name, t.data_ptr())
+        getattr(p, name + "_stride")[:] = _rows(t, q.shape if name == "q" else (B, k.shape[1], T, D), name)
+    return p
+
+
+def mikv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                          lse: Optional[torch.Tensor] = None, rules: Optional[ScoreRules] = None,
+                          scale: Optional[float] = None):
+    """Attention of whole prompts under ``rules`` (None: causal): q fp16 [B, Hq, T, 128], k, v fp16 [B, Hkv, T, 128]
+    -> out fp16 [B, Hq, T, 128], all with any strides (channels contiguous), and lse fp32 [B, Hq, T]."""
+    p = _prompt(q, k, v, scale)
+    _require(out, torch.float16, name="out")
+    stride = (c_int64 * 3)(*_rows(out, q.shape, "out"))
+    if lse is not None:
+        _require(lse, torch.float32, q.shape[:3], "lse")
+    r = None if rules is None else ctypes.byref(rules.desc(q.shape[1], (q.shape[0], q.shape[2])))
+    _check(lib().mikv_prompt_attention(ctypes.byref(p), r, out.data_ptr(), stride, _ptr(lse), _stream()),
+           "mikv_prompt_attention")
+
+
+def mikv_prompt_importance_workspace_size(batch: int, q_heads: int, kv_heads: int, tokens: int) -> int:
+    return int(lib().mikv_prompt_importance_workspace_size(batch, q_heads, kv_heads, tokens))
+
+
+def mikv_prompt_importance(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, scores: torch.Tensor,
+                           rules: Optional[ScoreRules] = None, scale: Optional[float] = None,
+                           workspace: Optional[torch.Tensor] = None):
+    """H2O importance of the prompt tokens under the rules of mikv_prompt_attention, from the lse that it wrote:
+    scores fp32 [B, Hkv, T]."""
+    p = _prompt(q, k, None, scale)
+    B, Hq, T, _ = q.shape
+    _require(lse, torch.float32, (B, Hq, T), "lse")
+    _require(scores, torch.float32, (B, k.shape[1], T), "scores")
+    ws = workspace
+    if ws is None:
+        ws = _workspace(mikv_prompt_importance_workspace_size(B, Hq, k.shape[1], T), q.device)
+    r = None if rules is None else ctypes.byref(rules.desc(Hq, (B, T)))
+    _check(lib().mikv_prompt_importance(ctypes.byref(p), r, _ptr(lse), _ptr(scores), _ptr(ws), ws.numel(), _stream()),
+           "mikv_prompt_importance")
 
 
 # -- the method's step sequence ---------------------------------------------------
