@@ -9,6 +9,22 @@
 
 namespace mikv {
 
+// Where one new token goes: the importance pool (rows, group parameters,
+// positions, scores), the position map and the status word, and the token's
+// key and value rows ([B * Hkv, 128] fp16) with the key balancer.
+struct AppendArgs {
+  uint8_t *hi_k, *hi_v;     // fp16 rows or INT8 codes
+  uint32_t *hi_kp, *hi_vp;  // (alpha, beta) pairs of INT8 rows
+  int32_t *hi_pos;
+  float *hi_acc;
+  uint8_t *map;             // nullable
+  int32_t *status;
+  const uint16_t *k, *v;    // the new token's rows
+  const float *balance;     // nullable (Eq. 3)
+  const float *score_init;  // nullable: initial score 0
+  int cap_hi, max_len, group, pos;
+};
+
 namespace {
 
 // Load 32 fp16 channels starting at `src` (16-byte aligned) into fp32,
@@ -67,22 +83,6 @@ __device__ inline void quantize_segment(const float x[32], int group, int lane4,
   if ((lane4 % (group / 32)) == 0) *param = (uint32_t)p.a16 | ((uint32_t)p.b16 << 16);
 }
 
-// Where one new token goes: the importance pool (rows, group parameters,
-// positions, scores), the position map and the status word, and the token's
-// key and value rows ([B * Hkv, 128] fp16) with the key balancer.
-struct AppendArgs {
-  uint8_t *hi_k, *hi_v;     // fp16 rows or INT8 codes
-  uint32_t *hi_kp, *hi_vp;  // (alpha, beta) pairs of INT8 rows
-  int32_t *hi_pos;
-  float *hi_acc;
-  uint8_t *map;             // nullable
-  int32_t *status;
-  const uint16_t *k, *v;    // the new token's rows
-  const float *balance;     // nullable (Eq. 3)
-  const float *score_init;  // nullable: initial score 0
-  int cap_hi, max_len, group, pos;
-};
-
 // Writes the new token of head h into importance-pool slot `slot` (an index
 // below cap_hi): 8 lanes, 0-3 the key row's 32-channel segments, 4-7 the
 // value row's; lane 0 also records the position, the initial score and the
@@ -95,6 +95,10 @@ __device__ inline void append_row(const AppendArgs &P, int h, int slot, int lane
   load_row_segment(lane_pick(is_v, P.v, P.k) + (int64_t)h * kHeadDim + lane4 * 32, bal, x);
   const int64_t row = (int64_t)h * P.cap_hi + slot;
   if constexpr (HI_BITS == 16) {
+    // fp16 of the fp32 product: the compiler would make the balanced key's product
+    // and its conversion one instruction that rounds once, straight to fp16
+#pragma unroll
+    for (int c = 0; c < 32; ++c) asm("" : "+v"(x[c]));
     uint32_t w[16];
 #pragma unroll
     for (int c = 0; c < 16; ++c) w[c] = pack_f16x2(x[2 * c], x[2 * c + 1]);
