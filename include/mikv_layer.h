@@ -98,7 +98,7 @@ int mikv_rotary(const mikv_heads *tensors, int32_t n, int32_t batch, int32_t tok
  * The score of query i and key j (positions) in query head h, and which keys
  * a query sees:
  *   s = scale q . k;  s = cap tanh(s / cap) if cap > 0;  s -= slopes[h] |i - j|;
- *   begin <= j < end.
+ *   begin <= j < end, and j > i - window if window > 0.
  * begin and end may hold any values (they are clamped to the sequence); where
  * begin >= end the query sees nothing: its output is 0, its log-sum-exp -inf.
  * K and V rows that a query does not see add nothing to it, whatever
@@ -109,6 +109,7 @@ typedef struct mikv_score_rules {
   const float *slopes;  /* fp32 [q_heads], finite; NULL: no bias */
   const int32_t *begin; /* prompt: [batch, tokens], decode: [batch]; NULL: 0 */
   const int32_t *end;   /* prompt: [batch, tokens], NULL: i + 1 (causal); decode: must be NULL */
+  int32_t window;       /* 0: none */
 } mikv_score_rules;
 
 /*
@@ -143,7 +144,7 @@ typedef struct mikv_prompt {
  *   rules  HOST pointer, or NULL: causal, no cap, no bias;
  *   out    fp16 [batch, q_heads, tokens, 128] through out_stride (as q's);
  *   lse    fp32 [batch, q_heads, tokens] or NULL: natural log of the sum of exp(s).
- * Errors: INVALID_ARG (NULL, counts < 1, q_heads % kv_heads, alignment, strides, scale, cap);
+ * Errors: INVALID_ARG (NULL, counts < 1, q_heads % kv_heads, alignment, strides, scale, cap, window);
  * UNSUPPORTED (head_dim, query heads per KV head, a token stride over 2^22, grids over 2^31).
  */
 int mikv_prompt_attention(const mikv_prompt *prompt, const mikv_score_rules *rules, uint16_t *out,
@@ -162,6 +163,26 @@ int mikv_prompt_attention(const mikv_prompt *prompt, const mikv_score_rules *rul
 size_t mikv_prompt_importance_workspace_size(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t tokens);
 int mikv_prompt_importance(const mikv_prompt *prompt, const mikv_score_rules *rules, const float *lse, float *scores,
                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * mikv_decode_attention and mikv_decode_step under score rules: the query is
+ * the token at position length - 1, a cached token's position is the one it
+ * was placed at, and `begin` (per sequence) hides earlier ones (left padding,
+ * an earlier document).  Hidden tokens have probability 0; a sequence that
+ * sees nothing gets an output of 0.
+ *   rules  HOST pointer; NULL: the unscored call.
+ * Other arguments, results, workspaces and errors as there; INVALID_ARG also for a
+ * negative or NaN cap, a negative window and for rules->end.
+ */
+int mikv_decode_attention_scored(const mikv_cache *c, int32_t length, const uint16_t *q, const float *balance,
+                                 float scale, const mikv_score_rules *rules, float *out, float *probs_hi,
+                                 float *probs_lo, int32_t flags, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+int mikv_decode_step_scored(const mikv_cache *c, int32_t length, const uint16_t *q, const uint16_t *k_new,
+                            const uint16_t *v_new, const float *balance, float scale, const mikv_score_rules *rules,
+                            float *out, float *probs_hi, float *probs_lo, int32_t k_heavy, int32_t window,
+                            int32_t flags, void *workspace, size_t workspace_bytes, void *const *phase_events,
+                            void *stream);
 
 #ifdef __cplusplus
 }

@@ -98,3 +98,30 @@ def prompt_attention(q, k, v, seen, scale, cap=0.0, slopes=None):
     used = seen.any(axis=0)
     clean = np.where((used & np.isfinite(v).all(axis=1))[:, None], v, 0.0)
     return p @ clean, lse, p
+
+
+def decode_attention(cache, q16, scale, begin, cap=0.0, slopes=None, window=0, balance=None):
+    """One token's attention over an OracleCache under score rules.
+
+    q16 fp16 [H, G, D]; begin int [H] (first visible position of each head's sequence);
+    slopes [H, G] or None; returns (o, p) fp64 [H, G, D], [H, G, L]."""
+    L = cache.length
+    o = np.zeros((cache.n_heads, cache.G, cache.d))
+    p = np.zeros((cache.n_heads, cache.G, L))
+    pos = np.arange(L)
+    for h in range(cache.n_heads):
+        k, v = (x.astype(np.float64) for x in cache.values(h))
+        q = np.asarray(q16[h], np.float16).astype(np.float32)
+        if balance is not None:
+            q = q / np.asarray(balance[h], np.float32)
+        seen = pos >= begin[h]
+        if window:
+            seen &= pos > L - 1 - window
+        if not cache.lo_bits:
+            seen &= cache.is_hi[h, :L]
+        for g in range(cache.G):
+            s = rule_scores(k @ q[g].astype(np.float64), scale, cap, 0.0 if slopes is None else float(slopes[h, g]),
+                            L - 1 - pos)
+            p[h, g], _ = masked_softmax(s, seen)
+            o[h, g] = p[h, g] @ np.where(seen[:, None], v, 0.0)
+    return o, p

@@ -8,7 +8,7 @@
 #include <cstdarg>
 #include <cstdio>
 
-#include "../../include/mikv.h"
+#include "../../include/mikv_layer.h"
 
 namespace mikv {
 
@@ -42,7 +42,9 @@ int validate_cache(const mikv_cache *c);
 // select), which with `appended` set counts that token into n_hi.
 int decode_partial(const mikv_cache *c, int32_t length, const uint16_t *q, const float *balance, float scale,
                    float *out, float *probs_hi, float *probs_lo, int32_t flags, void *ws, size_t ws_bytes,
-                   const uint16_t *k_new, const uint16_t *v_new, hipStream_t st);
+                   const uint16_t *k_new, const uint16_t *v_new, const mikv_score_rules *rules, hipStream_t st);
+// Score rules of a decode call (host side, before any launch).
+int check_decode_rules(const mikv_score_rules *r, const char *who);
 int decode_finalize_select(const mikv_cache *c, int32_t length, const uint16_t *q, const float *balance, float scale,
                            float *out, float *probs_hi, float *probs_lo, void *ws, size_t ws_bytes, int32_t k_heavy,
                            int32_t window, void *sel_ws, bool appended, hipStream_t st);
@@ -331,6 +333,25 @@ __device__ inline void store_int2_v(uint8_t *head_base, int64_t slot, int part, 
   for (int e = 0; e < 8; ++e)
     head_base[int2_v_byte(slot, 8 * part + e)] = (uint8_t)(((e < 4 ? lo : hi) >> (8 * (e & 3))) & 0xffu);
 }
+
+// ---------------------------------------------------------------------------
+// Device: tanh of score rules.
+// ---------------------------------------------------------------------------
+// Two forms: below kTanhSmall y + y^3 Q(y^2), Q of degree three fitted to (tanh y
+// / y - 1) / y^2 for the smallest largest error relative to tanh, 4.2e-8 (under one
+// fp32 half step); above it 1 - 2 / (1 + e^2y), within 2.5e-7 of 1.  The second one
+// would lose the scores' digits near 0, where scores far below their cap lie.
+constexpr float kTanhSmall = 0.55f;
+__device__ inline float tanh_small(float y) {
+  const float z = y * y;
+  const float q = fmaf(z, fmaf(z, fmaf(z, 0.016458744f, -0.052684136f), 0.13320942f), -0.33332959f);
+  return fmaf(z * y, q, y);
+}
+__device__ inline float tanh_any(float y) {
+  const float e = __builtin_amdgcn_exp2f(y * 2.8853900817779268f);  // e^2y
+  return fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + e), 1.0f);
+}
+__device__ inline float tanh_fine(float y) { return fabsf(y) < kTanhSmall ? tanh_small(y) : tanh_any(y); }
 
 // ---------------------------------------------------------------------------
 // Device: wave-level reductions (wave64).

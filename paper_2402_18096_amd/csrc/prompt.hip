@@ -42,6 +42,7 @@ struct PromptArgs {
   float *lse;
   const float *slopes;
   const int32_t *begin, *end;
+  int window;
   int q_heads, kv_heads, units, nblk, run, T;
   float scale, cap;  // scale: of the logit in log2 units (cap: to the argument of tanh); cap in log2 units
 };
@@ -85,11 +86,6 @@ __device__ inline u4_t read_v(const u4_t *tile, uint32_t off, int c, int kh) {
   return u4_t{x.x, x.y, y.x, y.y};
 }
 
-__device__ inline float tanh_of(float y) {
-  const float e = __builtin_amdgcn_exp2f(y * (2.0f * kLog2e));
-  return fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + e), 1.0f);
-}
-
 // How a tile's accumulators become scores in log2 units less the query's maximum:
 //   RAW:  x = fma(d, scale, fma(slope, row, base))     (cap: of tanh(d scale) instead of d, times cap)
 // with row the constant part of the key's index; an edge tile's accumulators
@@ -103,7 +99,7 @@ template <bool CAP, bool BIAS>
 __device__ inline float term(float d, int r, const Coef &c, float cap) {
   float a = c.base;
   if constexpr (BIAS) a = fmaf(c.slope, row_const(r), a);
-  if constexpr (CAP) return fmaf(tanh_of(d * c.scale), cap, a);
+  if constexpr (CAP) return fmaf(tanh_any(d * c.scale), cap, a);
   return fmaf(d, c.scale, a);
 }
 
@@ -150,9 +146,11 @@ __device__ inline int wave_min_int(int v) {
 __device__ inline int wave_max_int(int v) { return -wave_min_int(-v); }
 
 // A query's interval, clamped to the prompt; empty: (0, 0).
-__device__ inline void query_span(const int32_t *begin, const int32_t *end, int64_t at, int i, int T, int &lo, int &hi) {
+__device__ inline void query_span(const int32_t *begin, const int32_t *end, int window, int64_t at, int i, int T, int &lo,
+                                  int &hi) {
   lo = begin ? max(begin[at], 0) : 0;
   hi = end ? min(end[at], T) : i + 1;
+  if (window > 0) lo = max(lo, i + 1 - min(window, i + 1));
   if (lo >= hi) lo = hi = 0;
 }
 
@@ -184,7 +182,7 @@ void prompt_attention_kernel(PromptArgs A) {
     const uint16_t *r = qb + (int64_t)i * A.qs[2] + 8 * half;
 #pragma unroll
     for (int c = 0; c < 8; ++c) bq[cb][c] = *reinterpret_cast<const u4_t *>(r + 16 * c);
-    query_span(A.begin, A.end, (int64_t)b * T + i, i, T, lo[cb], hi[cb]);
+    query_span(A.begin, A.end, A.window, (int64_t)b * T + i, i, T, lo[cb], hi[cb]);
     full_lo[cb] = wave_max_int(lo[cb]);
     full_hi[cb] = wave_min_int(hi[cb]);
     any_lo = min(any_lo, wave_min_int(hi[cb] ? lo[cb] : T));
@@ -237,7 +235,7 @@ void prompt_attention_kernel(PromptArgs A) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = j0 + tile_row(r);
-        float s = CAP ? tanh_of(d[r] * A.scale) * A.cap : d[r] * A.scale;
+        float s = CAP ? tanh_any(d[r] * A.scale) * A.cap : d[r] * A.scale;
         if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own[cb] - j), s);
         d[r] = j >= lo[cb] && j < hi[cb] ? s : -kInf;
       }
@@ -445,6 +443,7 @@ struct SumArgs {
   const int32_t *begin, *end;
   const int4 *spans;  // of every 32 queries, or NULL (causal)
   float *scores;
+  int window;
   int q_heads, kv_heads, units, nblk, run, T;
   float scale, cap;
 };
@@ -452,10 +451,11 @@ struct SumArgs {
 // Interval extremes of 32 queries: smallest begin and largest end over those that
 // see something, largest begin and smallest end over all (the latter 0 if one
 // sees nothing).
-__global__ __launch_bounds__(64) void query_spans_kernel(const int32_t *begin, const int32_t *end, int T, int nsub, int4 *spans) {
+__global__ __launch_bounds__(64) void query_spans_kernel(const int32_t *begin, const int32_t *end, int window, int T, int nsub,
+                                                       int4 *spans) {
   const int b = blockIdx.y, i = blockIdx.x * 64 + threadIdx.x;
   int lo = 0, hi = 0;
-  if (i < T) query_span(begin, end, (int64_t)b * T + i, i, T, lo, hi);
+  if (i < T) query_span(begin, end, window, (int64_t)b * T + i, i, T, lo, hi);
   int a = hi ? lo : T, z = hi, x = lo, y = hi;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -542,7 +542,7 @@ void prompt_colsum_kernel(SumArgs A) {
       const int i = t * TR + tid, ic = min(i, T - 1);
       r_lse = A.lse[((int64_t)b * A.q_heads + kvh * G + g) * T + ic] * kLog2e;
       int lo, hi;
-      query_span(A.begin, A.end, (int64_t)b * T + ic, ic, T, lo, hi);
+      query_span(A.begin, A.end, A.window, (int64_t)b * T + ic, ic, T, lo, hi);
       r_span = i < T ? make_int2(lo, hi) : make_int2(0, 0);
     }
     if (tid < TR / 32) r_sub = sub_span(t * (TR / 32) + tid);
@@ -597,7 +597,7 @@ void prompt_colsum_kernel(SumArgs A) {
 #pragma unroll
               for (int r = 0; r < 16; ++r) {
                 const int j = j0 + tile_row(r);
-                float x = CAP ? tanh_of(d[r] * A.scale) * A.cap : d[r] * A.scale;
+                float x = CAP ? tanh_any(d[r] * A.scale) * A.cap : d[r] * A.scale;
                 if constexpr (BIAS) x = fmaf(-slope, (float)abs(i - j), x);
                 const float p = __builtin_amdgcn_exp2f(x - lse2);
                 cs[cb][r] += j >= span.x && j < span.y ? p : 0.0f;
@@ -661,6 +661,7 @@ int check_prompt(const char *who, const mikv_prompt *p, const mikv_score_rules *
   if (int e = check_rows(who, "k", p->k, p->k_stride)) return e;
   if (r) {
     if (!(r->cap >= 0.0f) || r->cap == kInf) return set_error(MIKV_ERR_INVALID_ARG, "%s: cap must be >= 0", who);
+    if (r->window < 0) return set_error(MIKV_ERR_INVALID_ARG, "%s: window must be >= 0", who);
     if (((uintptr_t)r->slopes | (uintptr_t)r->begin | (uintptr_t)r->end) % 4)
       return set_error(MIKV_ERR_INVALID_ARG, "%s: misaligned rules", who);
   }
@@ -705,7 +706,7 @@ extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rule
   PromptArgs A{};
   A.q = p->q, A.k = p->k, A.v = p->v, A.out = out, A.lse = lse;
   copy3(A.qs, p->q_stride), copy3(A.ks, p->k_stride), copy3(A.vs, p->v_stride), copy3(A.os, out_stride);
-  if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end;
+  if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end, A.window = rules->window;
   A.q_heads = p->q_heads, A.kv_heads = p->kv_heads, A.T = p->tokens;
   A.units = p->batch * p->kv_heads;
   A.nblk = (p->tokens + kBlockRows - 1) / kBlockRows;
@@ -738,17 +739,17 @@ extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rul
   SumArgs A{};
   A.q = p->q, A.k = p->k, A.lse = lse, A.scores = scores;
   copy3(A.qs, p->q_stride), copy3(A.ks, p->k_stride);
-  if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end;
+  if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end, A.window = rules->window;
   A.q_heads = p->q_heads, A.kv_heads = p->kv_heads, A.T = p->tokens;
   A.units = p->batch * p->kv_heads;
   score_scales(p->scale, rules ? rules->cap : 0.0f, A.scale, A.cap);
-  if (A.begin || A.end) {
+  if (A.begin || A.end || A.window) {
     const int nsub = (p->tokens + 31) / 32;
     A.spans = (const int4 *)ws;
     for (int b = 0; b < p->batch; b += 65535)
       hipLaunchKernelGGL(query_spans_kernel, dim3((p->tokens + 63) / 64, std::min(65535, p->batch - b)), dim3(64), 0, st,
                          A.begin ? A.begin + (int64_t)b * p->tokens : nullptr, A.end ? A.end + (int64_t)b * p->tokens : nullptr,
-                         p->tokens, nsub, (int4 *)ws + (int64_t)b * nsub);
+                         A.window, p->tokens, nsub, (int4 *)ws + (int64_t)b * nsub);
   }
   // waves on the same keys, by the blocks of 256 keys: as for the causal scores
   // (plan_pass), fewer keys per block only while the grid leaves CUs idle

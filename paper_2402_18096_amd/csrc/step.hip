@@ -27,12 +27,13 @@ extern "C" size_t mikv_decode_step_workspace_size(const mikv_cache *c, int32_t l
   return align256(a) + mikv_select_workspace_size(c);
 }
 
-extern "C" int mikv_decode_step(const mikv_cache *c, int32_t length, const uint16_t *q, const uint16_t *k_new,
-                                const uint16_t *v_new, const float *balance, float scale, float *out, float *probs_hi,
-                                float *probs_lo, int32_t k_heavy, int32_t window, int32_t flags, void *workspace,
-                                size_t workspace_bytes, void *const *phase_events, void *stream) {
+static int decode_step(const mikv_cache *c, int32_t length, const uint16_t *q, const uint16_t *k_new,
+                       const uint16_t *v_new, const float *balance, float scale, const mikv_score_rules *rules, float *out,
+                       float *probs_hi, float *probs_lo, int32_t k_heavy, int32_t window, int32_t flags, void *workspace,
+                       size_t workspace_bytes, void *const *phase_events, void *stream) {
   int rc = validate_cache(c);
   if (rc) return rc;
+  if ((rc = check_decode_rules(rules, "mikv_decode_step"))) return rc;
   if (!q || !k_new || !v_new || !out) return set_error(MIKV_ERR_INVALID_ARG, "mikv_decode_step: NULL input/output");
   if (length < 1 || length > c->max_len)
     return set_error(length < 1 ? MIKV_ERR_INVALID_ARG : MIKV_ERR_CAPACITY,
@@ -62,7 +63,8 @@ extern "C" int mikv_decode_step(const mikv_cache *c, int32_t length, const uint1
     // Two launches: the attention's partial phase, which also appends the
     // new token; then finalize, importance update and re-rank.
     mark(1);
-    rc = decode_partial(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, attn_ws, k_new, v_new, st);
+    rc = decode_partial(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, attn_ws, k_new, v_new, rules,
+                        st);
     if (rc) return rc;
     mark(2);
     rc = decode_finalize_select(c, length, q, balance, scale, out, probs_hi, probs_lo, ws, attn_ws, k_heavy, window,
@@ -78,7 +80,8 @@ extern "C" int mikv_decode_step(const mikv_cache *c, int32_t length, const uint1
     // Three launches: partial phase with the append, finalize with the
     // importance update, re-rank (which counts the new token into n_hi).
     mark(1);
-    rc = decode_partial(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, attn_ws, k_new, v_new, st);
+    rc = decode_partial(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, attn_ws, k_new, v_new, rules,
+                        st);
     if (rc) return rc;
     mark(2);
     rc = decode_finalize(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, attn_ws, true, st);
@@ -95,7 +98,7 @@ extern "C" int mikv_decode_step(const mikv_cache *c, int32_t length, const uint1
   if (rc) return rc;
   mark(1);
   rc = decode_partial(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, attn_ws, nullptr, nullptr,
-                      st);
+                      rules, st);
   if (rc) return rc;
   mark(2);
   rc = mikv_decode_attention_finalize(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, attn_ws,
@@ -109,6 +112,23 @@ extern "C" int mikv_decode_step(const mikv_cache *c, int32_t length, const uint1
   if (rc) return rc;
   mark(5);
   return MIKV_OK;
+}
+
+extern "C" int mikv_decode_step(const mikv_cache *c, int32_t length, const uint16_t *q, const uint16_t *k_new,
+                                const uint16_t *v_new, const float *balance, float scale, float *out, float *probs_hi,
+                                float *probs_lo, int32_t k_heavy, int32_t window, int32_t flags, void *workspace,
+                                size_t workspace_bytes, void *const *phase_events, void *stream) {
+  return decode_step(c, length, q, k_new, v_new, balance, scale, nullptr, out, probs_hi, probs_lo, k_heavy, window, flags,
+                     workspace, workspace_bytes, phase_events, stream);
+}
+
+extern "C" int mikv_decode_step_scored(const mikv_cache *c, int32_t length, const uint16_t *q, const uint16_t *k_new,
+                                       const uint16_t *v_new, const float *balance, float scale,
+                                       const mikv_score_rules *rules, float *out, float *probs_hi, float *probs_lo,
+                                       int32_t k_heavy, int32_t window, int32_t flags, void *workspace,
+                                       size_t workspace_bytes, void *const *phase_events, void *stream) {
+  return decode_step(c, length, q, k_new, v_new, balance, scale, rules, out, probs_hi, probs_lo, k_heavy, window, flags,
+                     workspace, workspace_bytes, phase_events, stream);
 }
 
 // ---------------------------------------------------------------------------

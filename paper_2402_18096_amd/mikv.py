@@ -103,7 +103,8 @@ class Heads(ctypes.Structure):
 
 class RulesDesc(ctypes.Structure):
     """Mirror of ``struct mikv_score_rules``."""
-    _fields_ = [("cap", c_float), ("slopes", c_void_p), ("begin", c_void_p), ("end", c_void_p)]
+    _fields_ = [("cap", c_float), ("slopes", c_void_p), ("begin", c_void_p), ("end", c_void_p),
+                ("window", c_int32)]
 
 
 class PromptDesc(ctypes.Structure):
@@ -125,6 +126,9 @@ _LAYER_SIGS = {
     "mikv_prompt_importance_workspace_size": (c_size_t, [c_int32, c_int32, c_int32, c_int32]),
     "mikv_prompt_importance": (c_int32, [_PP, _PR, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
 }
+
+for _n, _at in (("mikv_decode_attention", 5), ("mikv_decode_step", 7)):  # the rules follow the scale
+    _LAYER_SIGS[_n + "_scored"] = (c_int32, [*_SIGS[_n][1][:_at], _PR, *_SIGS[_n][1][_at:]])
 
 LAYER_EXPORTS = tuple(_LAYER_SIGS)
 
@@ -318,7 +322,7 @@ def mikv_quantize_kv(cache: MikvCache, k: torch.Tensor, v: torch.Tensor, pos0: i
            "mikv_quantize_kv")
 
 
-def _attention(name, cache, length, q, out, probs_hi, probs_lo, balance, scale, flags, workspace):
+def _attention(name, cache, length, q, out, probs_hi, probs_lo, balance, scale, flags, workspace, *rules):
     _require(q, torch.float16, (cache.batch, cache.q_heads, HEAD_DIM), "q")
     _require(out, torch.float32, (cache.batch, cache.q_heads, HEAD_DIM), "out")
     if probs_hi is not None:
@@ -329,7 +333,7 @@ def _attention(name, cache, length, q, out, probs_hi, probs_lo, balance, scale, 
     ws = workspace if workspace is not None else _workspace(L.mikv_decode_workspace_size(cache.ref(), length),
                                                             q.device)
     scale = 1.0 / math.sqrt(HEAD_DIM) if scale is None else scale
-    _check(getattr(L, name)(cache.ref(), length, _ptr(q), _ptr(balance), scale, _ptr(out), _ptr(probs_hi),
+    _check(getattr(L, name)(cache.ref(), length, _ptr(q), _ptr(balance), scale, *rules, _ptr(out), _ptr(probs_hi),
                             _ptr(probs_lo), flags, _ptr(ws), ws.numel(), _stream()), name)
 
 
@@ -430,11 +434,8 @@ def mikv_set_resident_bytes(nbytes: int) -> None:
     _check(lib().mikv_set_resident_bytes(int(nbytes)), "mikv_set_resident_bytes")
 
 
-def mikv_decode_step(cache: MikvCache, length: int, q, k_new, v_new, out, k_heavy: int, window: int,
-                     probs_hi=None, probs_lo=None, balance=None, scale=None, flags=0, workspace=None,
-                     phase_events=None):
-    """Whole decode step in one native call; ``phase_events`` is an optional
-    sequence of 6 ``torch.cuda.Event`` (already recorded once, so they exist)."""
+def _decode_step(name, cache, length, q, k_new, v_new, out, k_heavy, window, probs_hi, probs_lo, balance, scale, flags,
+                 workspace, phase_events, *rules):
     _require(q, torch.float16, (cache.batch, cache.q_heads, HEAD_DIM), "q")
     _require(k_new, torch.float16, (cache.batch, cache.kv_heads, HEAD_DIM), "k_new")
     _require(v_new, torch.float16, (cache.batch, cache.kv_heads, HEAD_DIM), "v_new")
@@ -446,9 +447,18 @@ def mikv_decode_step(cache: MikvCache, length: int, q, k_new, v_new, out, k_heav
     if phase_events is not None:
         ev = (c_void_p * 6)(*[e.cuda_event if e is not None else None for e in phase_events])
     scale = 1.0 / math.sqrt(HEAD_DIM) if scale is None else scale
-    _check(L.mikv_decode_step(cache.ref(), length, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(balance), scale,
-                              _ptr(out), _ptr(probs_hi), _ptr(probs_lo), k_heavy, window, flags, _ptr(ws),
-                              ws.numel(), ev, _stream()), "mikv_decode_step")
+    _check(getattr(L, name)(cache.ref(), length, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(balance), scale, *rules,
+                            _ptr(out), _ptr(probs_hi), _ptr(probs_lo), k_heavy, window, flags, _ptr(ws),
+                            ws.numel(), ev, _stream()), name)
+
+
+def mikv_decode_step(cache: MikvCache, length: int, q, k_new, v_new, out, k_heavy: int, window: int,
+                     probs_hi=None, probs_lo=None, balance=None, scale=None, flags=0, workspace=None,
+                     phase_events=None):
+    """Whole decode step in one native call; ``phase_events`` is an optional
+    sequence of 6 ``torch.cuda.Event`` (already recorded once, so they exist)."""
+    _decode_step("mikv_decode_step", cache, length, q, k_new, v_new, out, k_heavy, window, probs_hi, probs_lo, balance,
+                 scale, flags, workspace, phase_events)
 
 
 def mikv_decode_step_noalloc(cache: MikvCache, length: int, q, k_new, v_new, out, k_heavy: int, window: int,
@@ -539,11 +549,11 @@ def mikv_rotary(rotary: MikvRotary, xs, ys, positions: Optional[torch.Tensor] = 
 class ScoreRules:
     """Score rules of an attention (``struct mikv_score_rules``): tanh ``cap`` (0: none), ``slopes`` fp32 [Hq] of the
     bias by distance, and the keys that a query sees: ``begin``/``end`` int32 [B, T] of a prompt (mikv_mask_spans), or
-    ``begin`` int32 [B] of a decode step."""
+    ``begin`` int32 [B] of a decode step, and the last ``window`` (0: all)."""
 
     def __init__(self, cap: float = 0.0, slopes: Optional[torch.Tensor] = None, begin: Optional[torch.Tensor] = None,
-                 end: Optional[torch.Tensor] = None):
-        self.cap, self.slopes, self.begin, self.end = float(cap), slopes, begin, end
+                 end: Optional[torch.Tensor] = None, window: int = 0):
+        self.cap, self.slopes, self.begin, self.end, self.window = float(cap), slopes, begin, end, int(window)
 
     def desc(self, q_heads: int, span_shape) -> RulesDesc:
         if self.slopes is not None:
@@ -551,7 +561,7 @@ class ScoreRules:
         for name in ("begin", "end"):
             if getattr(self, name) is not None:
                 _require(getattr(self, name), torch.int32, span_shape, name)
-        return RulesDesc(self.cap, _ptr(self.slopes), _ptr(self.begin), _ptr(self.end))
+        return RulesDesc(self.cap, _ptr(self.slopes), _ptr(self.begin), _ptr(self.end), self.window)
 
 
 def mikv_mask_spans(begin: torch.Tensor, end: torch.Tensor, documents: Optional[torch.Tensor] = None,
@@ -622,6 +632,25 @@ def mikv_prompt_importance(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, 
            "mikv_prompt_importance")
 
 
+def _decode_rules(rules: Optional[ScoreRules], cache: MikvCache):
+    return None if rules is None else ctypes.byref(rules.desc(cache.q_heads, (cache.batch,)))
+
+
+def mikv_decode_attention_scored(cache, length, q, out, probs_hi=None, probs_lo=None, rules: Optional[ScoreRules] = None,
+                                 balance=None, scale=None, flags=0, workspace=None):
+    """mikv_decode_attention under score rules."""
+    _attention("mikv_decode_attention_scored", cache, length, q, out, probs_hi, probs_lo, balance, scale, flags, workspace,
+               _decode_rules(rules, cache))
+
+
+def mikv_decode_step_scored(cache: MikvCache, length: int, q, k_new, v_new, out, k_heavy: int, window: int,
+                            probs_hi=None, probs_lo=None, rules: Optional[ScoreRules] = None, balance=None, scale=None,
+                            flags=0, workspace=None, phase_events=None):
+    """mikv_decode_step under score rules."""
+    _decode_step("mikv_decode_step_scored", cache, length, q, k_new, v_new, out, k_heavy, window, probs_hi, probs_lo, balance,
+                 scale, flags, workspace, phase_events, _decode_rules(rules, cache))
+
+
 # -- the method's step sequence ---------------------------------------------------
 
 def heavy_budget(length: int, ratio_num: int, ratio_den: int, window: int, window_in_ratio: bool) -> int:
@@ -641,11 +670,19 @@ class MikvDecoder:
     (mikv_decode_attention, probabilities of both pools emitted), importance
     update (mikv_importance_update, or fused into attention with
     ``fused=True``) and re-rank/demote (mikv_select_topk).
+
+    With ``rotary`` the queries and keys of a step (and of :meth:`attend_prompt`)
+    are given as the projection leaves them, fp16, bf16 or fp32, and rotated to
+    their positions first.  ``rules`` (a cap, slopes, a window) apply to every attention.
     """
 
     def __init__(self, wl, max_len: Optional[int] = None, device="cuda", fused: bool = False,
-                 cap_slack: int = 64):
+                 cap_slack: int = 64, rotary: Optional[MikvRotary] = None, rules: Optional[ScoreRules] = None):
         self.wl, self.device, self.fused = wl, torch.device(device), fused
+        self.rotary = rotary
+        if rules is not None and (rules.begin is not None or rules.end is not None):
+            raise MikvError("MikvDecoder: begin and end come from the prompt's masks (attend_prompt)")
+        self.rules = self.step_rules = rules
         self.max_len = max_len or (wl.context + wl.steps)
         cap_hi = min(self.max_len, heavy_budget(self.max_len, wl.ratio_num, wl.ratio_den, wl.window,
                                                 wl.window_in_ratio) + wl.window + cap_slack)
@@ -665,6 +702,9 @@ class MikvDecoder:
         self.sel_ws = _workspace(L.mikv_select_workspace_size(c.ref()), self.device)
         sws = max(L.mikv_decode_step_workspace_size(c.ref(), n) for n in range(1, self.max_len + 1))
         self.step_ws = _workspace(sws, self.device)
+        if rotary is not None:  # the step's rotated rows
+            h = lambda n: torch.empty(B, n, 1, HEAD_DIM, dtype=torch.float16, device=self.device)
+            self._rotated = (h(Hq), h(wl.kv_heads), h(wl.kv_heads))
 
     def k_heavy(self, length: int) -> int:
         wl = self.wl
@@ -677,7 +717,10 @@ class MikvDecoder:
         q_prefill); q_prefill fp16 [B, Hq, T, D] (also when the workload
         balances keys and queries)."""
         wl, T = self.wl, k.shape[2]
+        self.step_rules = self.rules
         if scores is None:
+            if self.rules is not None:
+                raise MikvError("prefill: under rules the prompt's importance comes from attend_prompt")
             if q_prefill is None:
                 raise MikvError("prefill: the prompt's importance needs q_prefill")
             scores = torch.empty(wl.batch, wl.kv_heads, T, dtype=torch.float32, device=self.device)
@@ -690,6 +733,49 @@ class MikvDecoder:
         mikv_quantize_kv(self.cache, k, v, 0, self.balance, mask, scores)
         self.length = T
 
+    def attend_prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, documents: Optional[torch.Tensor] = None,
+                      prefix: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The whole prompt of the layer: rotary positions 0 .. T - 1 (with ``rotary``), attention under the rules and
+        the masks of ``documents`` and ``prefix`` (mikv_mask_spans), the prompt's importance under the same, and the cache
+        placed from it (:meth:`prefill`).  q [B, Hq, T, 128], k, v [B, Hkv, T, 128] with any strides (fp16, with
+        ``rotary`` also bf16 or fp32), e.g. views of a fused projection -> out fp16 [B, T, Hq, 128].
+
+        Every sequence ends at token T - 1 (shorter prompts are padded on the left, with a negative document id); the
+        tokens of later steps continue its last document and see it from its first token on."""
+        B, Hq, T, _ = q.shape
+        Hkv = k.shape[1]
+        rows = lambda n: torch.empty(B, n, T, HEAD_DIM, dtype=torch.float16, device=self.device)
+        if self.rotary is not None:
+            q, k, v = self._rotate((q, k, v), (rows(Hq), rows(Hkv), rows(Hkv)), 0)
+        else:
+            q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+        base = self.rules or ScoreRules()
+        begin = end = first = None
+        if documents is not None or prefix is not None:
+            begin, end = (torch.empty(B, T, dtype=torch.int32, device=self.device) for _ in range(2))
+            mikv_mask_spans(begin, end, documents, prefix)
+            first = begin[:, T - 1].contiguous()
+        rules = ScoreRules(base.cap, base.slopes, begin, end, base.window)
+        out = torch.empty(B, T, Hq, HEAD_DIM, dtype=torch.float16, device=self.device)
+        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=self.device)
+        mikv_prompt_attention(q, k, v, out.transpose(1, 2), lse, rules)
+        scores = torch.empty(B, Hkv, T, dtype=torch.float32, device=self.device)
+        mikv_prompt_importance(q, k, lse, scores, rules)
+        self.prefill(k, v, scores, q)
+        if first is not None:
+            self.step_rules = ScoreRules(base.cap, base.slopes, first, None, base.window)
+        return out
+
+    def _rotate(self, xs, ys, pos0: int):
+        mikv_rotary(self.rotary, xs, ys, pos0=pos0)
+        return ys
+
+    def _rotate_step(self, q, k_new, v_new):
+        if self.rotary is None:
+            return q, k_new, v_new
+        return [y.squeeze(2) for y in
+                self._rotate([x.unsqueeze(2) for x in (q, k_new, v_new)], self._rotated, self.length)]
+
     def step(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, emit_lo: bool = True,
              after_attention=None, emit_heavy: bool = False):
         """One decode step; q fp16 [B, Hq, D], k_new/v_new fp16 [B, Hkv, D].
@@ -698,12 +784,17 @@ class MikvDecoder:
         with ``emit_heavy`` the re-rank also writes the sorted heavy-token
         list to ``self.heavy_idx`` [B, Hkv, k_heavy]."""
         c = self.cache
+        q, k_new, v_new = self._rotate_step(q, k_new, v_new)
         mikv_quantize_kv(c, k_new.unsqueeze(2), v_new.unsqueeze(2), self.length, self.balance)
         self.length += 1
         L = self.length
         flags = ATTN_ACCUMULATE if self.fused else 0
-        mikv_decode_attention(c, L, q, self.out, self.probs_hi, self.probs_lo if emit_lo else None,
-                              self.balance, None, flags, self.attn_ws)
+        lo = self.probs_lo if emit_lo else None
+        if self.step_rules is not None:
+            mikv_decode_attention_scored(c, L, q, self.out, self.probs_hi, lo, self.step_rules, self.balance, None, flags,
+                                         self.attn_ws)
+        else:
+            mikv_decode_attention(c, L, q, self.out, self.probs_hi, lo, self.balance, None, flags, self.attn_ws)
         if after_attention is not None:
             after_attention()
         if not self.fused:
@@ -719,9 +810,14 @@ class MikvDecoder:
     def step_native(self, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, emit_lo: bool = True,
                     phase_events=None):
         """The same decode step as :meth:`step`, launched by one native call."""
+        q, k_new, v_new = self._rotate_step(q, k_new, v_new)
         self.length += 1
         L = self.length
-        mikv_decode_step(self.cache, L, q, k_new, v_new, self.out, self.k_heavy(L), self.wl.window, self.probs_hi,
-                         self.probs_lo if emit_lo else None, self.balance, None,
-                         ATTN_ACCUMULATE if self.fused else 0, self.step_ws, phase_events)
+        lo, flags = self.probs_lo if emit_lo else None, ATTN_ACCUMULATE if self.fused else 0
+        if self.step_rules is not None:
+            mikv_decode_step_scored(self.cache, L, q, k_new, v_new, self.out, self.k_heavy(L), self.wl.window,
+                                    self.probs_hi, lo, self.step_rules, self.balance, None, flags, self.step_ws, phase_events)
+        else:
+            mikv_decode_step(self.cache, L, q, k_new, v_new, self.out, self.k_heavy(L), self.wl.window, self.probs_hi,
+                             lo, self.balance, None, flags, self.step_ws, phase_events)
         return self.out
