@@ -150,7 +150,10 @@ __device__ inline bool rule_positions(const RuleArgs &R) { return R.slopes || R.
 // 2^(cls(p) - 24) for codes (exact fp16 subnormals), or the stored fp16
 // values for BITS == 16.
 // ---------------------------------------------------------------------------
-template <int BITS>
+// FINE: 2-, 3- and 4-bit codes moved up to mantissa bits 6-9 (classes 6 and 8).
+// The dot products multiply the deepest subnormals at reduced precision (scores
+// of 2-bit keys 3e-6 off against 2e-7 with FINE); a shift more for every four codes.
+template <int BITS, bool FINE = false>
 struct Fmt {
   static constexpr bool kQuant = BITS != 16;
   __host__ __device__ static constexpr int lo(int p) {
@@ -163,8 +166,12 @@ struct Fmt {
     return BITS == 16 || BITS == 3 ? 2 * p + 1 : lo(p) + (BITS == 8 ? 2 : BITS == 4 ? 4 : 8);
   }
   __host__ __device__ static constexpr int cls(int p) {
+    if (FINE) return BITS == 2 ? 6 + 2 * (p % 2) : BITS == 3 || BITS == 4 ? 6 : 0;
     return BITS == 4 ? 4 * (p % 2) : BITS == 2 ? 2 * (p % 4) : 0;
   }
+  // largest and smallest class
+  static constexpr int kMaxCls = FINE ? (BITS == 2 ? 8 : BITS == 3 || BITS == 4 ? 6 : 0) : BITS == 2 ? 6 : BITS == 4 ? 4 : 0;
+  static constexpr int kMinCls = FINE && BITS <= 4 ? 6 : 0;
   template <int CPL>
   __device__ static inline void unpack(const uint32_t *raw, uint32_t *out) {
     if constexpr (BITS == 16) {
@@ -180,14 +187,38 @@ struct Fmt {
       for (int j = 0; j < CPL / 2; ++j) {
         const int bit = 6 * j, wi = bit / 32, sh = bit % 32;
         const uint64_t win = ((uint64_t)(wi + 1 < KW ? raw[wi + 1] : 0u) << 32) | raw[wi];
-        const uint32_t x = (uint32_t)(win >> sh);
-        out[j] = (x & 7u) | (((x >> 3) & 7u) << 16);
+        if constexpr (FINE) {
+          const uint32_t x = (uint32_t)(sh >= 6 ? win >> (sh - 6) : win << (6 - sh));
+          out[j] = (x & 0x1c0u) | ((x << 13) & 0x01c00000u);
+        } else {
+          const uint32_t x = (uint32_t)(win >> sh);
+          out[j] = (x & 7u) | (((x >> 3) & 7u) << 16);
+        }
       }
     } else if constexpr (BITS == 8) {
 #pragma unroll
       for (int j = 0; j < CPL / 4; ++j) {
         out[2 * j] = raw[j] & 0x00ff00ffu;
         out[2 * j + 1] = (raw[j] >> 8) & 0x00ff00ffu;
+      }
+    } else if constexpr (FINE && BITS == 4) {
+#pragma unroll
+      for (int j = 0; j < CPL / 8; ++j) {
+        const uint32_t x = raw[j];
+        out[4 * j] = (x << 6) & 0x03c003c0u;
+        out[4 * j + 1] = (x << 2) & 0x03c003c0u;
+        out[4 * j + 2] = (x >> 2) & 0x03c003c0u;
+        out[4 * j + 3] = (x >> 6) & 0x03c003c0u;
+      }
+    } else if constexpr (FINE) {
+#pragma unroll
+      for (int j = 0; j < CPL / 16; ++j) {
+        const uint32_t x = raw[j], s[4] = {x << 6, x << 2, x >> 2, x >> 6};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          out[8 * j + 2 * k] = s[k] & 0x00c000c0u;
+          out[8 * j + 2 * k + 1] = s[k] & 0x03000300u;
+        }
       }
     } else if constexpr (BITS == 4) {
 #pragma unroll
@@ -222,13 +253,14 @@ __device__ inline half2_t as_h2(uint32_t u) { return __builtin_bit_cast(half2_t,
 // = the format's largest cls: never below 1, exact in fp16.  A wave whose
 // largest |q_hat| would overflow fp16 that way keeps shift 0.  The shift is
 // undone in the score scale (wave-uniform).
-template <int MAXCLS>
+// (smallest class MINCLS: the largest factor is 2^(MAXCLS - MINCLS).)
+template <int MAXCLS, int MINCLS = 0>
 __device__ inline int query_shift(float qmax_lane) {
-  if constexpr (MAXCLS == 0) {
-    return 0;
+  if constexpr (MAXCLS == MINCLS) {
+    return MAXCLS;
   } else {
     const float m = wave_max(qmax_lane);
-    return m * (float)(1 << MAXCLS) < 60000.0f ? MAXCLS : 0;
+    return m * (float)(1 << (MAXCLS - MINCLS)) < 60000.0f ? MAXCLS : MINCLS;
   }
 }
 
@@ -343,6 +375,7 @@ __device__ inline void load_seg_rows(Rows<BITS, CPL> &r, rsrc_t rk, rsrc_t rv, r
 template <int BITS, int G, int CPL, bool SPLITQ, int UNROLL, int PREFETCH, bool KPC = false, bool STREAM = false, bool RULES = false>
 __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, bool is_hi, float *s_lds) {
   using F = Fmt<BITS>;
+  using FK = Fmt<BITS, RULES && !KPC>;  // keys (the per-channel ones enter fp32 FMAs, which are exact)
   constexpr int LPT = kHeadDim / CPL, TPW = 64 / LPT, NP = CPL / 2;
   constexpr bool Q = F::kQuant;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -490,7 +523,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
       bal[4 * j + 3] = v.w;
     }
   }
-  constexpr int kMaxCls = BITS == 2 ? 6 : BITS == 4 ? 4 : 0;
+  constexpr int kMaxCls = FK::kMaxCls, kMinCls = FK::kMinCls;
   int qshift = 0;
   if constexpr (kMaxCls > 0 && !KPC) {
     // bound on |q_hat| over the wave: max |q| / min b
@@ -510,7 +543,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
       for (int c = 1; c < CPL; ++c) bmin = fminf(bmin, bal[c]);
       bound = bound / bmin;
     }
-    qshift = query_shift<kMaxCls>(bound);
+    qshift = query_shift<kMaxCls, kMinCls>(bound);
   }
   const float s2scale_q = Q ? __builtin_ldexpf(s2scale, 24 - qshift) : s2scale;
   float arg_scale = 0.0f, slope2[RULES ? G : 1];
@@ -548,7 +581,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
     qsum24[i] = __builtin_ldexpf(s, qshift - 24);
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      const float sc = __builtin_ldexpf(1.0f, qshift - F::cls(p));
+      const float sc = __builtin_ldexpf(1.0f, qshift - FK::cls(p));
       const float a = qhat(F::lo(p)) * sc, bb = qhat(F::hi(p)) * sc;
       const _Float16 ah = (_Float16)a, bh = (_Float16)bb;
       qh[i][p] = half2_t{ah, bh};
@@ -611,7 +644,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
       if constexpr (RULES) valid[u] = valid[u] && (int)cur[u].pos >= begin;
       uint32_t kx[NP], kraw[Rows<BITS, CPL>::KW];
       seg_words(cur[u].k, kraw);
-      F::template unpack<CPL>(kraw, kx);
+      FK::template unpack<CPL>(kraw, kx);
       const half2_t kab = as_h2(cur[u].kp);  // (alpha, beta) of the key group
       if constexpr (KPC) {
         // the token's key block (the parameter word is its position); tokens
