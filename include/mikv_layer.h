@@ -105,7 +105,7 @@ int mikv_rotary(const mikv_heads *tensors, int32_t n, int32_t batch, int32_t tok
  * they hold, NaN and infinities included.
  */
 typedef struct mikv_score_rules {
-  float cap;            /* 0: none */
+  float cap;            /* 0: none; finite, and scale / cap within fp32's normal range */
   const float *slopes;  /* fp32 [q_heads], finite; NULL: no bias */
   const int32_t *begin; /* prompt: [batch, tokens], decode: [batch]; NULL: 0 */
   const int32_t *end;   /* prompt: [batch, tokens], NULL: i + 1 (causal); decode: must be NULL */

@@ -618,10 +618,17 @@ extern "C" size_t mikv_decode_workspace_size(const mikv_cache *c, int32_t length
 
 namespace mikv {
 
-int check_decode_rules(const mikv_score_rules *r, const char *who) {
+int check_cap(float cap, float scale, const char *who) {
+  if (!(cap >= 0.0f) || cap == __builtin_huge_valf())
+    return set_error(MIKV_ERR_INVALID_ARG, "%s: cap must be >= 0 and finite", who);
+  if (cap > 0.0f && scale / cap < 0x1p-126f)
+    return set_error(MIKV_ERR_INVALID_ARG, "%s: scale / cap is below the fp32 range", who);
+  return MIKV_OK;
+}
+
+int check_decode_rules(const mikv_score_rules *r, float scale, const char *who) {
   if (!r) return MIKV_OK;
-  if (!(r->cap >= 0.0f) || r->cap == __builtin_huge_valf())
-    return set_error(MIKV_ERR_INVALID_ARG, "%s: cap must be >= 0", who);
+  if (int e = check_cap(r->cap, scale, who)) return e;
   if (r->end) return set_error(MIKV_ERR_INVALID_ARG, "%s: a decode step takes no end", who);
   if (r->window < 0) return set_error(MIKV_ERR_INVALID_ARG, "%s: window must be >= 0", who);
   if (((uintptr_t)r->slopes | (uintptr_t)r->begin) % 4)
@@ -771,7 +778,7 @@ extern "C" int mikv_decode_attention(const mikv_cache *c, int32_t length, const 
 extern "C" int mikv_decode_attention_scored(const mikv_cache *c, int32_t length, const uint16_t *q, const float *balance,
                                             float scale, const mikv_score_rules *rules, float *out, float *probs_hi,
                                             float *probs_lo, int32_t flags, void *ws, size_t ws_bytes, void *stream) {
-  int rc = check_decode_rules(rules, "mikv_decode_attention_scored");
+  int rc = check_decode_rules(rules, scale, "mikv_decode_attention_scored");
   if (rc) return rc;
   rc = decode_partial(c, length, q, balance, scale, out, probs_hi, probs_lo, flags, ws, ws_bytes, nullptr, nullptr, rules,
                       (hipStream_t)stream);

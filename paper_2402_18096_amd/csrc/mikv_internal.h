@@ -44,7 +44,8 @@ int decode_partial(const mikv_cache *c, int32_t length, const uint16_t *q, const
                    float *out, float *probs_hi, float *probs_lo, int32_t flags, void *ws, size_t ws_bytes,
                    const uint16_t *k_new, const uint16_t *v_new, const mikv_score_rules *rules, hipStream_t st);
 // Score rules of a decode call (host side, before any launch).
-int check_decode_rules(const mikv_score_rules *r, const char *who);
+int check_cap(float cap, float scale, const char *who);
+int check_decode_rules(const mikv_score_rules *r, float scale, const char *who);
 int decode_finalize_select(const mikv_cache *c, int32_t length, const uint16_t *q, const float *balance, float scale,
                            float *out, float *probs_hi, float *probs_lo, void *ws, size_t ws_bytes, int32_t k_heavy,
                            int32_t window, void *sel_ws, bool appended, hipStream_t st);
@@ -342,10 +343,10 @@ __device__ inline void store_int2_v(uint8_t *head_base, int64_t slot, int part, 
 // fp32 half step); above it 1 - 2 / (1 + e^2y), within 2.5e-7 of 1.  The second one
 // would lose the scores' digits near 0, where scores far below their cap lie.
 constexpr float kTanhSmall = 0.55f;
+constexpr float kTanhQ0 = -0.33332959f, kTanhQ1 = 0.13320942f, kTanhQ2 = -0.052684136f, kTanhQ3 = 0.016458744f;
 __device__ inline float tanh_small(float y) {
   const float z = y * y;
-  const float q = fmaf(z, fmaf(z, fmaf(z, 0.016458744f, -0.052684136f), 0.13320942f), -0.33332959f);
-  return fmaf(z * y, q, y);
+  return fmaf(z * y, fmaf(z, fmaf(z, fmaf(z, kTanhQ3, kTanhQ2), kTanhQ1), kTanhQ0), y);
 }
 __device__ inline float tanh_any(float y) {
   const float e = __builtin_amdgcn_exp2f(y * 2.8853900817779268f);  // e^2y

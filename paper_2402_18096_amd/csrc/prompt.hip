@@ -31,9 +31,12 @@ namespace mikv {
 namespace {
 
 constexpr int kTileKeys = 64;           // keys per LDS tile
-constexpr int kBlockRows = 4 * kWaveRows;
 constexpr float kRaise = 1024.0f;       // raise a query's maximum when a lane's 16 weights of a tile sum past this
 constexpr float kInf = __builtin_huge_valf();
+
+struct CapPoly {
+  float c0, c1, c2, c3, c4, limit;  // P's coefficients, and the largest |d| it holds for
+};
 
 struct PromptArgs {
   const uint16_t *q, *k, *v;
@@ -45,13 +48,14 @@ struct PromptArgs {
   int window;
   int q_heads, kv_heads, units, nblk, run, T;
   float scale, cap;  // scale: of the logit in log2 units (cap: to the argument of tanh); cap in log2 units
+  CapPoly poly;
 };
 
 typedef int16_t s4_t __attribute__((ext_vector_type(4)));
 
-// The rows of a streamed tile straight to LDS (each wave instruction moves four
+// The rows of a streamed tile straight to LDS, by NW waves (each wave instruction moves four
 // rows), zeros past the prompt.  SWZ(row) is XORed into a row's 16-byte word index.
-template <class Swz>
+template <int NW, class Swz>
 __device__ inline void stage_rows(u4_t *lds, const uint16_t *rows, int64_t stride, int row0, int T, Swz swz) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = 4 * wave + (lane >> 4), have = min(kTileKeys, T - row0);
@@ -59,12 +63,12 @@ __device__ inline void stage_rows(u4_t *lds, const uint16_t *rows, int64_t strid
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(rows + (int64_t)row0 * stride), (short)0,
                                         have > 0 ? (int)((have - 1) * stride * 2 + kHeadDim * 2) : 0, 0x00020000);
 #pragma unroll
-  for (int u = 0; u < kTileKeys / 16; ++u) {
-    const int r = row + 16 * u;
+  for (int u = 0; u < kTileKeys / (4 * NW); ++u) {
+    const int r = row + 4 * NW * u;
     // (a row past the prompt: past the descriptor whatever the stride)
     const uint32_t off = r < have ? (uint32_t)r * (uint32_t)(stride * 2) + 16u * (uint32_t)((lane & 15) ^ swz(r)) : 0x7ffffff0u;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        rsrc, (__attribute__((address_space(3))) void *)(lds + (16 * u + 4 * wave) * kRowWords), 16, off, 0, 0, 0);
+        rsrc, (__attribute__((address_space(3))) void *)(lds + (4 * NW * u + 4 * wave) * kRowWords), 16, off, 0, 0, 0);
   }
 }
 // K: 16 lanes read one word of 16 rows; V: 32 lanes read 32 bytes of four rows twice.
@@ -87,21 +91,36 @@ __device__ inline u4_t read_v(const u4_t *tile, uint32_t off, int c, int kh) {
 }
 
 // How a tile's accumulators become scores in log2 units less the query's maximum:
-//   RAW:  x = fma(d, scale, fma(slope, row, base))     (cap: of tanh(d scale) instead of d, times cap)
-// with row the constant part of the key's index; an edge tile's accumulators
-// hold final scores (scale 1, slope 0, no cap).
+//   x = fma(d, P(d^2), fma(slope, row, base))
+// with row the constant part of the key's index, and P the logit's scale alone
+// without a cap.  CAP: where all of a tile's |d| leave tanh's argument below
+// kTanhSmall, cap tanh(d arg) = d P(d^2) with P of degree four (tanh_small, its
+// coefficients scaled by cap and arg once): five FMAs and a product per logit instead
+// of an exponential and a reciprocal (16 cycles each) beside three of them.  A tile
+// that some query does not see whole, or with a larger |d|, is given its final
+// scores in the accumulators first (edge), and P = 1, no slope.
 struct Coef {
-  float scale, slope, base;
+  float slope, base, scale;
+  CapPoly p;
 };
 __host__ __device__ constexpr float row_const(int r) { return (float)(8 * (r >> 2) + (r & 3)); }
 
 template <bool CAP, bool BIAS>
-__device__ inline float term(float d, int r, const Coef &c, float cap) {
+__device__ inline float term(float d, int r, const Coef &c) {
   float a = c.base;
   if constexpr (BIAS) a = fmaf(c.slope, row_const(r), a);
-  if constexpr (CAP) return fmaf(tanh_any(d * c.scale), cap, a);
+  if constexpr (CAP) {
+    const float u = d * d;
+    return fmaf(d, fmaf(u, fmaf(u, fmaf(u, fmaf(u, c.p.c4, c.p.c3), c.p.c2), c.p.c1), c.p.c0), a);
+  }
   return fmaf(d, c.scale, a);
 }
+// The score of a key that a query does not see.  With a cap the accumulators are
+// squared: a finite number whose square is finite, below every other score
+// (those end at kLowest) as -inf is.
+constexpr float kLowest = -1e18f;
+template <bool CAP>
+constexpr float hidden_score() { return CAP ? -1.5e19f : -__builtin_huge_valf(); }
 
 __device__ inline uint32_t pack2(float a, float b) {
   typedef _Float16 h2 __attribute__((ext_vector_type(2)));
@@ -114,24 +133,26 @@ __device__ inline uint32_t pack2(float a, float b) {
 // returned.  ahead(i) issues LDS reads after the i-th pair of MFMAs.
 template <bool CAP, bool BIAS, class Ahead>
 __device__ inline float stage(f16_t &next, const u4_t (&key)[8], const u4_t (&query)[8], f16_t (&out)[4],
-                              u4_t (&vt)[4][2], const u4_t (&w)[2], const f16_t &cur, const Coef &c, float cap, u4_t (&p)[2],
+                              u4_t (&vt)[4][2], const u4_t (&w)[2], const f16_t &cur, const Coef &c, u4_t (&p)[2],
                               Ahead ahead) {
   f16_t d = splat(0.0f);
   float ts[2] = {0.0f, 0.0f};
-  float x0 = term<CAP, BIAS>(cur[0], 0, c, cap), x1 = term<CAP, BIAS>(cur[1], 1, c, cap);
+  float x0 = term<CAP, BIAS>(cur[0], 0, c), x1 = term<CAP, BIAS>(cur[1], 1, c);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     d = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(key[i]), as_h8(query[i]), d, 0, 0, 0);
     out[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vt[i & 3][i >> 2]), as_h8(w[i >> 2]), out[i & 3], 0, 0, 0);
     ahead(i);
-    const float p0 = __builtin_amdgcn_exp2f(x0), p1 = __builtin_amdgcn_exp2f(x1);
+    float p0 = __builtin_amdgcn_exp2f(x0), p1 = __builtin_amdgcn_exp2f(x1);
     if (i < 7) {
-      x0 = term<CAP, BIAS>(cur[2 * i + 2], 2 * i + 2, c, cap);
-      x1 = term<CAP, BIAS>(cur[2 * i + 3], 2 * i + 3, c, cap);
+      x0 = term<CAP, BIAS>(cur[2 * i + 2], 2 * i + 2, c);
+      x1 = term<CAP, BIAS>(cur[2 * i + 3], 2 * i + 3, c);
     }
     ts[0] += p0;
     ts[1] += p1;
-    p[i >> 2][i & 3] = pack2(p0, p1);
+    uint32_t w2 = pack2(p0, p1);
+    asm volatile("" : "+v"(w2), "+v"(ts[0]), "+v"(ts[1]));  // here: the compiler would move all this behind the MFMAs
+    p[i >> 2][i & 3] = w2;
     __builtin_amdgcn_sched_barrier(0);
   }
   next = d;
@@ -154,20 +175,24 @@ __device__ inline void query_span(const int32_t *begin, const int32_t *end, int 
   if (lo >= hi) lo = hi = 0;
 }
 
-template <bool CAP, bool BIAS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
+// A block of NW waves: min(G, NW) query heads of one KV head's group times the
+// 64-query tiles that fill it, so that its waves need the same keys as nearly as
+// they can.
+template <bool CAP, bool BIAS, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void prompt_attention_kernel(PromptArgs A) {
   constexpr int TR = kTileKeys;
   __shared__ u4_t s_k[2][TR * kRowWords];
   __shared__ u4_t s_v[3][TR * kRowWords];
-  __shared__ int s_span[4][2];
+  int(*s_span)[2] = reinterpret_cast<int(*)[2]>(s_v[2]);  // free until the third tile
   const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = A.q_heads / A.kv_heads, T = A.T;
+  const int hw = min(G, NW), rw = NW / hw, groups = G / hw;  // heads and row tiles of a block, head groups
   int hk, idx;
-  if (!block_unit(A.units, A.nblk * G, A.run, hk, idx)) return;
-  const int b = hk / A.kv_heads, kvh = hk % A.kv_heads, head = kvh * G + idx % G;
-  const int i_wave = (A.nblk - 1 - idx / G) * kBlockRows + kWaveRows * wave;
+  if (!block_unit(A.units, A.nblk * groups, A.run, hk, idx)) return;
+  const int b = hk / A.kv_heads, kvh = hk % A.kv_heads, head = kvh * G + (idx % groups) * hw + wave % hw;
+  const int i_wave = kWaveRows * ((A.nblk - 1 - idx / groups) * rw + wave / hw);
   const uint16_t *kb = A.k + b * A.ks[0] + kvh * A.ks[1], *vb = A.v + b * A.vs[0] + kvh * A.vs[1];
   const uint16_t *qb = A.q + b * A.qs[0] + head * A.qs[1];
 
@@ -182,6 +207,10 @@ void prompt_attention_kernel(PromptArgs A) {
     const uint16_t *r = qb + (int64_t)i * A.qs[2] + 8 * half;
 #pragma unroll
     for (int c = 0; c < 8; ++c) bq[cb][c] = *reinterpret_cast<const u4_t *>(r + 16 * c);
+    // in the accumulation registers, from which the MFMAs read them (the others
+    // are full; without this they are copied back for every use)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) asm volatile("" : "+a"(bq[cb][c]));
     query_span(A.begin, A.end, A.window, (int64_t)b * T + i, i, T, lo[cb], hi[cb]);
     full_lo[cb] = wave_max_int(lo[cb]);
     full_hi[cb] = wave_min_int(hi[cb]);
@@ -194,7 +223,7 @@ void prompt_attention_kernel(PromptArgs A) {
   }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < NW; ++w) {
     any_lo = min(any_lo, s_span[w][0]);
     any_hi = max(any_hi, s_span[w][1]);
   }
@@ -211,21 +240,37 @@ void prompt_attention_kernel(PromptArgs A) {
     for (int c = 0; c < 4; ++c) o[cb][c] = splat(0.0f);
 
   if (t_first < t_end) {
+    const int seen_lo = max(full_lo[0], full_lo[1]), seen_hi = min(full_hi[0], full_hi[1]);  // by every query of the wave
     const int i_lo[2] = {min(i_wave, T - 1), min(i_wave + 32, T - 1)};
     const int i_hi[2] = {min(i_wave + 31, T - 1), min(i_wave + 63, T - 1)};
     // whether every query of tile cb sees keys j0 .. j0 + 31, on one side of it where the bias needs that
-    auto full = [&](int cb, int j0) {
+    // (and, with a cap, whether its polynomial holds for the whole tile)
+    auto full = [&](const f16_t &d, int cb, int j0) {
       bool f = j0 >= full_lo[cb] && j0 + 32 <= full_hi[cb];
       if constexpr (BIAS) f = f && (j0 + 31 <= i_lo[cb] || j0 > i_hi[cb]);
+      if constexpr (CAP) {
+        float big = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(d[r]));
+        f = f && !__ballot(!(big < A.poly.limit));
+      }
       return f;
     };
-    auto coef = [&](int cb, int j0) {
+    auto coef = [&](bool is_full, int cb, int j0) {
       Coef c;
-      c.scale = A.scale;
       c.slope = 0.0f;
       c.base = -m[cb];
+      if constexpr (CAP) {
+        c.p.c0 = is_full ? A.poly.c0 : 1.0f;
+        c.p.c1 = is_full ? A.poly.c1 : 0.0f;
+        c.p.c2 = is_full ? A.poly.c2 : 0.0f;
+        c.p.c3 = is_full ? A.poly.c3 : 0.0f;
+        c.p.c4 = is_full ? A.poly.c4 : 0.0f;
+      } else {
+        c.scale = is_full ? A.scale : 1.0f;
+      }
       if constexpr (BIAS) {
-        c.slope = j0 > i_hi[cb] ? -slope : slope;
+        c.slope = !is_full ? 0.0f : j0 > i_hi[cb] ? -slope : slope;
         c.base = fmaf(c.slope, (float)(j0 + 4 * half - i_own[cb]), c.base);
       }
       return c;
@@ -235,9 +280,10 @@ void prompt_attention_kernel(PromptArgs A) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = j0 + tile_row(r);
-        float s = CAP ? tanh_any(d[r] * A.scale) * A.cap : d[r] * A.scale;
+        float s = CAP ? tanh_fine(d[r] * A.scale) * A.cap : d[r] * A.scale;
         if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own[cb] - j), s);
-        d[r] = j >= lo[cb] && j < hi[cb] ? s : -kInf;
+        if constexpr (CAP) s = s < kLowest ? kLowest : s;
+        d[r] = j >= lo[cb] && j < hi[cb] ? s : hidden_score<CAP>();
       }
     };
     // Where a tile's weights sum past kRaise (or are NaN: the maximum starts at
@@ -245,14 +291,13 @@ void prompt_attention_kernel(PromptArgs A) {
     // The two lanes of a query keep one maximum.
     auto settle = [&](const f16_t &d, bool is_full, int cb, int j0, float ts, u4_t (&p)[2]) {
       if (__ballot(!(ts <= kRaise))) {
-        Coef c = coef(cb, j0);
-        c.base += m[cb] == -kInf ? -kInf : m[cb];
-        if (m[cb] == -kInf) c.base = BIAS && is_full ? c.slope * (float)(j0 + 4 * half - i_own[cb]) : 0.0f;
-        if (!is_full) c.base = 0.0f;
+        Coef c = coef(is_full, cb, j0);
+        c.base = BIAS ? c.slope * (float)(j0 + 4 * half - i_own[cb]) : 0.0f;
         float s[16], mx = -kInf;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = is_full ? term<CAP, BIAS>(d[r], r, c, A.cap) : d[r];
+          s[r] = term<CAP, BIAS>(d[r], r, c);
+          if (CAP && s[r] < 5.0f * kLowest) s[r] = -kInf;
           mx = fmaxf(mx, s[r]);
         }
         mx = fmaxf(m[cb], fmaxf(mx, __shfl_xor(mx, 32, 64)));
@@ -278,8 +323,8 @@ void prompt_attention_kernel(PromptArgs A) {
 
     const uint32_t off = tile_offset(), voff = v_offset();
     auto load_tile = [&](int t) {
-      stage_rows(s_k[(t - t_first) & 1], kb, A.ks[2], t * TR, T, swz_k);
-      stage_rows(s_v[(t - t_first) % 3], vb, A.vs[2], t * TR, T, swz_v);
+      stage_rows<NW>(s_k[(t - t_first) & 1], kb, A.ks[2], t * TR, T, swz_k);
+      stage_rows<NW>(s_v[(t - t_first) % 3], vb, A.vs[2], t * TR, T, swz_v);
     };
     load_tile(t_first);
     if (t_first + 1 < t_end) load_tile(t_first + 1);
@@ -334,7 +379,7 @@ void prompt_attention_kernel(PromptArgs A) {
           for (int r = 0; r < 16; ++r) o[cb][c][r] += hits[r] > 0.0f ? __builtin_nanf("") : 0.0f;
         }
     };
-    f16_t d0, d1 = splat(-kInf);
+    f16_t d0, d1 = splat(hidden_score<CAP>());
     bool full1 = false, bad = false;
     int j1 = t_first * TR;
     const int n_sub = 2 * (t_end - t_first);
@@ -344,13 +389,10 @@ void prompt_attention_kernel(PromptArgs A) {
       // before, weights of the second query tile before
       float ts;
       auto none = [](int) {};
-      if (CAP && !full1)
-        ts = stage<false, false>(d0, kf, bq[0], o[0], vf, p0, d1, Coef{1.0f, 0.0f, -m[1]}, A.cap, p1, none);
-      else
-        ts = stage<CAP, BIAS>(d0, kf, bq[0], o[0], vf, p0, d1, full1 ? coef(1, j1) : Coef{1.0f, 0.0f, -m[1]}, A.cap, p1, none);
+      ts = stage<CAP, BIAS>(d0, kf, bq[0], o[0], vf, p0, d1, coef(full1, 1, j1), p1, none);
       settle(d1, full1, 1, j1, ts, p1);
       if (bad) poison(s - 1, p0, p1);
-      const bool full0 = full(0, j0);
+      const bool full0 = full(d0, 0, j0);
       if (!full0) edge(d0, 0, j0);
       // the last subtile of a tile: the next tile is complete, and every wave is
       // done with this tile's keys and the value rows of the one before
@@ -366,24 +408,21 @@ void prompt_attention_kernel(PromptArgs A) {
         kf[i] = read_word(kn, off, kr, i);
         vf[i & 3][i >> 2] = read_v(vn, voff, i & 3, i >> 2);
       };
-      if (CAP && !full0)
-        ts = stage<false, false>(d1, kf, bq[1], o[1], vf, p1, d0, Coef{1.0f, 0.0f, -m[0]}, A.cap, p0, ahead);
-      else
-        ts = stage<CAP, BIAS>(d1, kf, bq[1], o[1], vf, p1, d0, full0 ? coef(0, j0) : Coef{1.0f, 0.0f, -m[0]}, A.cap, p0, ahead);
+      ts = stage<CAP, BIAS>(d1, kf, bq[1], o[1], vf, p1, d0, coef(full0, 0, j0), p0, ahead);
       if ((s & 1) && t_first + t + 2 < t_end) load_tile(t_first + t + 2);
       settle(d0, full0, 0, j0, ts, p0);
-      full1 = full(1, j0);
+      full1 = full(d1, 1, j0);
       j1 = j0;
       if (!full1) edge(d1, 1, j0);
-      bad = !(full0 && full1) && clean();
+      bad = !(j0 >= seen_lo && j0 + 32 <= seen_hi) && clean();
     }
     // the weights of the last second query tile, and both last value products
     {
-      const Coef c = full1 ? coef(1, j1) : Coef{1.0f, 0.0f, -m[1]};
+      const Coef c = coef(full1, 1, j1);
       float ts = 0.0f, x[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        x[r] = __builtin_amdgcn_exp2f(full1 ? term<CAP, BIAS>(d1[r], r, c, A.cap) : d1[r] + c.base);
+        x[r] = __builtin_amdgcn_exp2f(term<CAP, BIAS>(d1[r], r, c));
         ts += x[r];
       }
 #pragma unroll
@@ -401,7 +440,9 @@ void prompt_attention_kernel(PromptArgs A) {
   // out = O / l, through LDS so that whole rows are stored
   wait_loads();
   __syncthreads();
-  u4_t *rows = wave < 2 ? s_k[wave] : s_v[wave - 2];  // 16 KiB each
+  u4_t *rows = s_k[0] + wave * (kWaveRows * kRowWords);  // 16 KiB each, s_k and on into s_v
+  static_assert(NW <= 2 || sizeof(s_k) == 2 * kWaveRows * kRowWords * 16, "two waves' rows fill s_k");
+  if (NW > 2 && wave >= 2) rows = s_v[wave - 2];
 #pragma unroll
   for (int cb = 0; cb < 2; ++cb) {
     const float sum = l[cb] + __shfl_xor(l[cb], 32, 64);
@@ -446,6 +487,7 @@ struct SumArgs {
   int window;
   int q_heads, kv_heads, units, nblk, run, T;
   float scale, cap;
+  CapPoly poly;
 };
 
 // Interval extremes of 32 queries: smallest begin and largest end over those that
@@ -537,7 +579,7 @@ void prompt_colsum_kernel(SumArgs A) {
     const uint16_t *rows = qb + g * A.qs[1];
 #pragma unroll
     for (int u = 0; u < TR / 64; ++u)
-      stage_rows(s_rows[buf] + 64 * u * kRowWords, rows, A.qs[2], t * TR + 64 * u, T, swz_k);
+      stage_rows<4>(s_rows[buf] + 64 * u * kRowWords, rows, A.qs[2], t * TR + 64 * u, T, swz_k);
     if (tid < TR) {
       const int i = t * TR + tid, ic = min(i, T - 1);
       r_lse = A.lse[((int64_t)b * A.q_heads + kvh * G + g) * T + ic] * kLog2e;
@@ -585,19 +627,25 @@ void prompt_colsum_kernel(SumArgs A) {
             const f16_t d = logits(ak[cb], bq);
             bool full = j0 >= full_lo && j0 + 32 <= full_hi;
             if constexpr (BIAS) full = full && (j0 + 31 <= i0 || j0 > i0 + 31);
+            if constexpr (CAP) {
+              float big = 0.0f;
+#pragma unroll
+              for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(d[r]));
+              full = full && !__ballot(!(big < A.poly.limit));
+            }
             if (full) {
-              Coef c = {A.scale, 0.0f, -lse2};
+              Coef c = {0.0f, -lse2, A.scale, A.poly};
               if constexpr (BIAS) {
                 c.slope = j0 > i0 ? -slope : slope;
                 c.base = fmaf(c.slope, (float)(j0 + 4 * half - i), c.base);
               }
 #pragma unroll
-              for (int r = 0; r < 16; ++r) cs[cb][r] += __builtin_amdgcn_exp2f(term<CAP, BIAS>(d[r], r, c, A.cap));
+              for (int r = 0; r < 16; ++r) cs[cb][r] += __builtin_amdgcn_exp2f(term<CAP, BIAS>(d[r], r, c));
             } else {
 #pragma unroll
               for (int r = 0; r < 16; ++r) {
                 const int j = j0 + tile_row(r);
-                float x = CAP ? tanh_any(d[r] * A.scale) * A.cap : d[r] * A.scale;
+                float x = CAP ? tanh_fine(d[r] * A.scale) * A.cap : d[r] * A.scale;
                 if constexpr (BIAS) x = fmaf(-slope, (float)abs(i - j), x);
                 const float p = __builtin_amdgcn_exp2f(x - lse2);
                 cs[cb][r] += j >= span.x && j < span.y ? p : 0.0f;
@@ -660,7 +708,7 @@ int check_prompt(const char *who, const mikv_prompt *p, const mikv_score_rules *
   if (int e = check_rows(who, "q", p->q, p->q_stride)) return e;
   if (int e = check_rows(who, "k", p->k, p->k_stride)) return e;
   if (r) {
-    if (!(r->cap >= 0.0f) || r->cap == kInf) return set_error(MIKV_ERR_INVALID_ARG, "%s: cap must be >= 0", who);
+    if (int e = check_cap(r->cap, p->scale, who)) return e;
     if (r->window < 0) return set_error(MIKV_ERR_INVALID_ARG, "%s: window must be >= 0", who);
     if (((uintptr_t)r->slopes | (uintptr_t)r->begin | (uintptr_t)r->end) % 4)
       return set_error(MIKV_ERR_INVALID_ARG, "%s: misaligned rules", who);
@@ -668,10 +716,20 @@ int check_prompt(const char *who, const mikv_prompt *p, const mikv_score_rules *
   return MIKV_OK;
 }
 
-// log2 units: s log2(e) = scale' d, or cap' tanh(scale' d)
-void score_scales(float scale, float cap, float &s, float &c) {
-  c = cap * kLog2e;
-  s = cap > 0.0f ? scale / cap : scale * kLog2e;
+// log2 units: s log2(e) = scale' d, or cap' tanh(scale' d) = d P(d^2) up to poly.limit
+template <class Args>
+void score_scales(float scale, float cap, Args &A) {
+  A.cap = cap * kLog2e;
+  A.scale = cap > 0.0f ? scale / cap : scale * kLog2e;
+  if (cap > 0.0f) {
+    const double a = (double)scale / cap, z = a * a, c = (double)scale * kLog2e;
+    A.poly.c0 = (float)c;
+    A.poly.c1 = (float)(c * z * kTanhQ0);
+    A.poly.c2 = (float)(c * z * z * kTanhQ1);
+    A.poly.c3 = (float)(c * z * z * z * kTanhQ2);
+    A.poly.c4 = (float)(c * z * z * z * z * kTanhQ3);
+    A.poly.limit = (float)(kTanhSmall / a);
+  }
 }
 
 unsigned grid_blocks(int units, int per_unit, int run) {
@@ -680,6 +738,17 @@ unsigned grid_blocks(int units, int per_unit, int run) {
 
 template <class T>
 void copy3(T d[3], const T s[3]) { d[0] = s[0], d[1] = s[1], d[2] = s[2]; }
+
+template <int NW>
+void launch_attention(PromptArgs &A, int G, bool cap, bool bias, hipStream_t st) {
+  const int hw = std::min(G, NW), rows = kWaveRows * (NW / hw), per_unit = (A.T + rows - 1) / rows * (G / hw);
+  A.nblk = (A.T + rows - 1) / rows;
+  A.run = (int)std::min<int64_t>((int64_t)A.units * per_unit >= 4096 ? 32 : 4, per_unit);
+  const dim3 grid(grid_blocks(A.units, per_unit, A.run));
+  auto kernel = cap ? (bias ? prompt_attention_kernel<true, true, NW> : prompt_attention_kernel<true, false, NW>)
+                    : (bias ? prompt_attention_kernel<false, true, NW> : prompt_attention_kernel<false, false, NW>);
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), 0, st, A);
+}
 
 template <int WS>
 void launch_colsum(const SumArgs &A, dim3 grid, hipStream_t st) {
@@ -709,15 +778,10 @@ extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rule
   if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end, A.window = rules->window;
   A.q_heads = p->q_heads, A.kv_heads = p->kv_heads, A.T = p->tokens;
   A.units = p->batch * p->kv_heads;
-  A.nblk = (p->tokens + kBlockRows - 1) / kBlockRows;
-  const int per_unit = A.nblk * (p->q_heads / p->kv_heads);
-  A.run = std::min((int64_t)A.units * per_unit >= 4096 ? 32 : 4, per_unit);
-  score_scales(p->scale, rules ? rules->cap : 0.0f, A.scale, A.cap);
-  const dim3 grid(grid_blocks(A.units, per_unit, A.run));
+  const int G = p->q_heads / p->kv_heads;
+  score_scales(p->scale, rules ? rules->cap : 0.0f, A);
   const bool cap = A.cap > 0.0f, bias = A.slopes != nullptr;
-  auto kernel = cap ? (bias ? prompt_attention_kernel<true, true> : prompt_attention_kernel<true, false>)
-                    : (bias ? prompt_attention_kernel<false, true> : prompt_attention_kernel<false, false>);
-  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, A);
+  launch_attention<4>(A, G, cap, bias, (hipStream_t)stream);
   return check_launch(who);
 }
 
@@ -742,7 +806,7 @@ extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rul
   if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end, A.window = rules->window;
   A.q_heads = p->q_heads, A.kv_heads = p->kv_heads, A.T = p->tokens;
   A.units = p->batch * p->kv_heads;
-  score_scales(p->scale, rules ? rules->cap : 0.0f, A.scale, A.cap);
+  score_scales(p->scale, rules ? rules->cap : 0.0f, A);
   if (A.begin || A.end || A.window) {
     const int nsub = (p->tokens + 31) / 32;
     A.spans = (const int4 *)ws;

@@ -33,7 +33,7 @@ static int decode_step(const mikv_cache *c, int32_t length, const uint16_t *q, c
                        size_t workspace_bytes, void *const *phase_events, void *stream) {
   int rc = validate_cache(c);
   if (rc) return rc;
-  if ((rc = check_decode_rules(rules, "mikv_decode_step"))) return rc;
+  if ((rc = check_decode_rules(rules, scale, "mikv_decode_step"))) return rc;
   if (!q || !k_new || !v_new || !out) return set_error(MIKV_ERR_INVALID_ARG, "mikv_decode_step: NULL input/output");
   if (length < 1 || length > c->max_len)
     return set_error(length < 1 ? MIKV_ERR_INVALID_ARG : MIKV_ERR_CAPACITY,
