@@ -35,7 +35,7 @@ constexpr float kRaise = 1024.0f;       // raise a query's maximum when a lane's
 constexpr float kInf = __builtin_huge_valf();
 
 struct CapPoly {
-  float c0, c1, c2, c3, c4, limit;  // P's coefficients, and the largest |d| it holds for
+  float c0, c1, c2, c3, c4, limit;  // P's coefficients, and the |d| below which it holds
 };
 
 struct PromptArgs {
@@ -53,23 +53,32 @@ struct PromptArgs {
 
 typedef int16_t s4_t __attribute__((ext_vector_type(4)));
 
-// The rows of a streamed tile straight to LDS, by NW waves (each wave instruction moves four
-// rows), zeros past the prompt.  SWZ(row) is XORed into a row's 16-byte word index.
+// The rows of a streamed tile straight to LDS, by NW waves (each wave instruction
+// moves four rows), zeros past the prompt (past the descriptor's end, where rows do
+// not overlap).  SWZ(row) is XORed into a row's 16-byte word index; a lane's
+// offsets are the same for every tile.
+template <int NW>
+constexpr int kLoads = kTileKeys / (4 * NW);
 template <int NW, class Swz>
-__device__ inline void stage_rows(u4_t *lds, const uint16_t *rows, int64_t stride, int row0, int T, Swz swz) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = 4 * wave + (lane >> 4), have = min(kTileKeys, T - row0);
+__device__ inline void row_offsets(uint32_t (&off)[kLoads<NW>], int64_t stride, Swz swz) {
+  const int lane = threadIdx.x & 63, row = 4 * (threadIdx.x >> 6) + (lane >> 4);
+#pragma unroll
+  for (int u = 0; u < kLoads<NW>; ++u) {
+    const int r = row + 4 * NW * u;
+    off[u] = (uint32_t)r * (uint32_t)(stride * 2) + 16u * (uint32_t)((lane & 15) ^ swz(r));
+  }
+}
+template <int NW>
+__device__ inline void stage_rows(u4_t *lds, const uint16_t *rows, int64_t stride, int row0, int T,
+                                  const uint32_t (&off)[kLoads<NW>]) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), have = min(kTileKeys, T - row0);
   const __amdgpu_buffer_rsrc_t rsrc =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(rows + (int64_t)row0 * stride), (short)0,
                                         have > 0 ? (int)((have - 1) * stride * 2 + kHeadDim * 2) : 0, 0x00020000);
 #pragma unroll
-  for (int u = 0; u < kTileKeys / (4 * NW); ++u) {
-    const int r = row + 4 * NW * u;
-    // (a row past the prompt: past the descriptor whatever the stride)
-    const uint32_t off = r < have ? (uint32_t)r * (uint32_t)(stride * 2) + 16u * (uint32_t)((lane & 15) ^ swz(r)) : 0x7ffffff0u;
+  for (int u = 0; u < kLoads<NW>; ++u)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        rsrc, (__attribute__((address_space(3))) void *)(lds + (4 * NW * u + 4 * wave) * kRowWords), 16, off, 0, 0, 0);
-  }
+        rsrc, (__attribute__((address_space(3))) void *)(lds + (4 * NW * u + 4 * wave) * kRowWords), 16, off[u], 0, 0, 0);
 }
 // K: 16 lanes read one word of 16 rows; V: 32 lanes read 32 bytes of four rows twice.
 __device__ inline int swz_k(int r) { return r & 15; }
@@ -97,10 +106,10 @@ __device__ inline u4_t read_v(const u4_t *tile, uint32_t off, int c, int kh) {
 // kTanhSmall, cap tanh(d arg) = d P(d^2) with P of degree four (tanh_small, its
 // coefficients scaled by cap and arg once): five FMAs and a product per logit instead
 // of an exponential and a reciprocal (16 cycles each) beside three of them.  A tile
-// that some query does not see whole, or with a larger |d|, is given its final
-// scores in the accumulators first (edge), and P = 1, no slope.
+// that some query does not see whole is given its final scores in the
+// accumulators first (edge), and P = 1, no slope; one with a larger |d| is weighed again (settle).
 struct Coef {
-  float slope, base, scale;
+  float slope, base, scale, limit;
   CapPoly p;
 };
 __host__ __device__ constexpr float row_const(int r) { return (float)(8 * (r >> 2) + (r & 3)); }
@@ -130,13 +139,14 @@ __device__ inline uint32_t pack2(float a, float b) {
 
 // One half step: the logits `next` = key x query, the value product out += vt x w
 // and, between their MFMAs, the weights `p` of the tile `cur`, whose sum is
-// returned.  ahead(i) issues LDS reads after the i-th pair of MFMAs.
+// returned (CAP: infinite where a |d| is past the polynomial's limit).  ahead(i) issues
+// LDS reads after the i-th pair of MFMAs.
 template <bool CAP, bool BIAS, class Ahead>
 __device__ inline float stage(f16_t &next, const u4_t (&key)[8], const u4_t (&query)[8], f16_t (&out)[4],
                               u4_t (&vt)[4][2], const u4_t (&w)[2], const f16_t &cur, const Coef &c, u4_t (&p)[2],
                               Ahead ahead) {
   f16_t d = splat(0.0f);
-  float ts[2] = {0.0f, 0.0f};
+  float ts[2] = {0.0f, 0.0f}, big = 0.0f;
   float x0 = term<CAP, BIAS>(cur[0], 0, c), x1 = term<CAP, BIAS>(cur[1], 1, c);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -151,12 +161,13 @@ __device__ inline float stage(f16_t &next, const u4_t (&key)[8], const u4_t (&qu
     ts[0] += p0;
     ts[1] += p1;
     uint32_t w2 = pack2(p0, p1);
-    asm volatile("" : "+v"(w2), "+v"(ts[0]), "+v"(ts[1]));  // here: the compiler would move all this behind the MFMAs
+    if constexpr (CAP) big = fmaxf(big, fmaxf(fabsf(cur[2 * i]), fabsf(cur[2 * i + 1])));
+    asm volatile("" : "+v"(w2), "+v"(ts[0]), "+v"(ts[1]), "+v"(big));  // here: the compiler would move all this behind the MFMAs
     p[i >> 2][i & 3] = w2;
     __builtin_amdgcn_sched_barrier(0);
   }
   next = d;
-  return ts[0] + ts[1];
+  return CAP && !(big < c.limit) ? kInf : ts[0] + ts[1];
 }
 
 __device__ inline int wave_min_int(int v) {
@@ -217,6 +228,7 @@ void prompt_attention_kernel(PromptArgs A) {
     any_lo = min(any_lo, wave_min_int(hi[cb] ? lo[cb] : T));
     any_hi = max(any_hi, wave_max_int(hi[cb]));
   }
+  const int own_lo = any_lo, own_hi = any_hi;
   if (lane == 0) {
     s_span[wave][0] = any_lo;
     s_span[wave][1] = any_hi;
@@ -244,16 +256,9 @@ void prompt_attention_kernel(PromptArgs A) {
     const int i_lo[2] = {min(i_wave, T - 1), min(i_wave + 32, T - 1)};
     const int i_hi[2] = {min(i_wave + 31, T - 1), min(i_wave + 63, T - 1)};
     // whether every query of tile cb sees keys j0 .. j0 + 31, on one side of it where the bias needs that
-    // (and, with a cap, whether its polynomial holds for the whole tile)
-    auto full = [&](const f16_t &d, int cb, int j0) {
+    auto full = [&](int cb, int j0) {
       bool f = j0 >= full_lo[cb] && j0 + 32 <= full_hi[cb];
       if constexpr (BIAS) f = f && (j0 + 31 <= i_lo[cb] || j0 > i_hi[cb]);
-      if constexpr (CAP) {
-        float big = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(d[r]));
-        f = f && !__ballot(!(big < A.poly.limit));
-      }
       return f;
     };
     auto coef = [&](bool is_full, int cb, int j0) {
@@ -266,6 +271,7 @@ void prompt_attention_kernel(PromptArgs A) {
         c.p.c2 = is_full ? A.poly.c2 : 0.0f;
         c.p.c3 = is_full ? A.poly.c3 : 0.0f;
         c.p.c4 = is_full ? A.poly.c4 : 0.0f;
+        c.limit = is_full ? A.poly.limit : kInf;
       } else {
         c.scale = is_full ? A.scale : 1.0f;
       }
@@ -287,8 +293,8 @@ void prompt_attention_kernel(PromptArgs A) {
       }
     };
     // Where a tile's weights sum past kRaise (or are NaN: the maximum starts at
-    // -inf) in any lane: raise the maxima, rescale, and weigh the tile again.
-    // The two lanes of a query keep one maximum.
+    // -inf; or not valid, see stage) in any lane: raise the maxima, rescale, and
+    // weigh the tile again.  The two lanes of a query keep one maximum.
     auto settle = [&](const f16_t &d, bool is_full, int cb, int j0, float ts, u4_t (&p)[2]) {
       if (__ballot(!(ts <= kRaise))) {
         Coef c = coef(is_full, cb, j0);
@@ -296,8 +302,12 @@ void prompt_attention_kernel(PromptArgs A) {
         float s[16], mx = -kInf;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[r] = term<CAP, BIAS>(d[r], r, c);
-          if (CAP && s[r] < 5.0f * kLowest) s[r] = -kInf;
+          if constexpr (CAP) {
+            s[r] = is_full ? fmaf(tanh_fine(d[r] * A.scale), A.cap, BIAS ? fmaf(c.slope, row_const(r), c.base) : 0.0f)
+                           : d[r] < 5.0f * kLowest ? -kInf : d[r];
+          } else {
+            s[r] = term<CAP, BIAS>(d[r], r, c);
+          }
           mx = fmaxf(mx, s[r]);
         }
         mx = fmaxf(m[cb], fmaxf(mx, __shfl_xor(mx, 32, 64)));
@@ -322,15 +332,40 @@ void prompt_attention_kernel(PromptArgs A) {
     };
 
     const uint32_t off = tile_offset(), voff = v_offset();
+    uint32_t k_off[kLoads<NW>], v_off[kLoads<NW>];
+    row_offsets<NW>(k_off, A.ks[2], swz_k);
+    row_offsets<NW>(v_off, A.vs[2], swz_v);
     auto load_tile = [&](int t) {
-      stage_rows<NW>(s_k[(t - t_first) & 1], kb, A.ks[2], t * TR, T, swz_k);
-      stage_rows<NW>(s_v[(t - t_first) % 3], vb, A.vs[2], t * TR, T, swz_v);
+      stage_rows<NW>(s_k[(t - t_first) & 1], kb, A.ks[2], t * TR, T, k_off);
+      stage_rows<NW>(s_v[(t - t_first) % 3], vb, A.vs[2], t * TR, T, v_off);
     };
     load_tile(t_first);
     if (t_first + 1 < t_end) load_tile(t_first + 1);
     wait_loads();
     __syncthreads();
 
+    // The subtiles that any query of this wave sees; for the others it only keeps
+    // step with the block.
+    const int s_first = own_hi > own_lo ? own_lo / 32 - 2 * t_first : 0;
+    const int s_last = own_hi > own_lo ? (own_hi + 31) / 32 - 2 * t_first : 0;
+    const int n_sub = 2 * (t_end - t_first);
+    // The last subtile of a tile: the next tile is complete, and every wave is
+    // done with this tile's keys and the value rows of the one before (turn); then the
+    // tile after the next may be loaded (refill), after this one's LDS reads: the
+    // compiler holds LDS reads back for loads to LDS that are under way.
+    auto turn = [&](int s) {
+      if (s & 1) {
+        wait_loads();
+        __syncthreads();
+      }
+    };
+    auto refill = [&](int s) {
+      if ((s & 1) && t_first + (s >> 1) + 2 < t_end) load_tile(t_first + (s >> 1) + 2);
+    };
+    for (int s = 0; s < s_first; ++s) {
+      turn(s);
+      refill(s);
+    }
     // Before the first subtile: weights and value operands of zero, and a second
     // tile that sees nothing (edge form), with its first key.
     u4_t kf[8], vf[4][2], p0[2], p1[2];
@@ -338,7 +373,7 @@ void prompt_attention_kernel(PromptArgs A) {
     for (int i = 0; i < 8; ++i) vf[i & 3][i >> 2] = u4_t{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 2; ++i) p0[i] = p1[i] = u4_t{0, 0, 0, 0};
-    read_tile(s_k[0], off, 0, kf);
+    read_tile(s_k[(s_first >> 1) & 1], off, 32 * (s_first & 1), kf);
     // A value of a row that some query does not see must not reach that query as
     // 0 x NaN: in an edge subtile infinities and NaN are taken out of the value
     // operand (clean says whether any were there), and the queries that do see
@@ -382,8 +417,7 @@ void prompt_attention_kernel(PromptArgs A) {
     f16_t d0, d1 = splat(hidden_score<CAP>());
     bool full1 = false, bad = false;
     int j1 = t_first * TR;
-    const int n_sub = 2 * (t_end - t_first);
-    for (int s = 0; s < n_sub; ++s) {
+    for (int s = s_first; s < s_last; ++s) {
       const int t = s >> 1, j0 = t_first * TR + 32 * s;
       // stage 1: logits of the first query tile, value product of its tile
       // before, weights of the second query tile before
@@ -392,14 +426,9 @@ void prompt_attention_kernel(PromptArgs A) {
       ts = stage<CAP, BIAS>(d0, kf, bq[0], o[0], vf, p0, d1, coef(full1, 1, j1), p1, none);
       settle(d1, full1, 1, j1, ts, p1);
       if (bad) poison(s - 1, p0, p1);
-      const bool full0 = full(d0, 0, j0);
+      const bool full0 = full(0, j0);
       if (!full0) edge(d0, 0, j0);
-      // the last subtile of a tile: the next tile is complete, and every wave is
-      // done with this tile's keys and the value rows of the one before
-      if (s & 1) {
-        wait_loads();
-        __syncthreads();
-      }
+      turn(s);
       // stage 2: the same for the second query tile, the weights of the first;
       // the next subtile's keys and this one's value rows are read on the way
       const u4_t *kn = s_k[((s + 1) >> 1) & 1], *vn = s_v[t % 3] + 32 * (s & 1) * kRowWords;
@@ -409,9 +438,9 @@ void prompt_attention_kernel(PromptArgs A) {
         vf[i & 3][i >> 2] = read_v(vn, voff, i & 3, i >> 2);
       };
       ts = stage<CAP, BIAS>(d1, kf, bq[1], o[1], vf, p1, d0, coef(full0, 0, j0), p0, ahead);
-      if ((s & 1) && t_first + t + 2 < t_end) load_tile(t_first + t + 2);
+      refill(s);
       settle(d0, full0, 0, j0, ts, p0);
-      full1 = full(d1, 1, j0);
+      full1 = full(1, j0);
       j1 = j0;
       if (!full1) edge(d1, 1, j0);
       bad = !(j0 >= seen_lo && j0 + 32 <= seen_hi) && clean();
@@ -419,21 +448,27 @@ void prompt_attention_kernel(PromptArgs A) {
     // the weights of the last second query tile, and both last value products
     {
       const Coef c = coef(full1, 1, j1);
-      float ts = 0.0f, x[16];
+      float ts = 0.0f, big = 0.0f, x[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         x[r] = __builtin_amdgcn_exp2f(term<CAP, BIAS>(d1[r], r, c));
         ts += x[r];
+        big = fmaxf(big, fabsf(d1[r]));
       }
+      if (CAP && !(big < c.limit)) ts = kInf;
 #pragma unroll
       for (int i = 0; i < 8; ++i) p1[i >> 2][i & 3] = pack2(x[2 * i], x[2 * i + 1]);
       settle(d1, full1, 1, j1, ts, p1);
-      if (bad) poison(n_sub - 1, p0, p1);
+      if (bad) poison(s_last - 1, p0, p1);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       o[0][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p0[i >> 2]), o[0][i & 3], 0, 0, 0);
       o[1][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p1[i >> 2]), o[1][i & 3], 0, 0, 0);
+    }
+    for (int s = s_last; s < n_sub; ++s) {
+      turn(s);
+      refill(s);
     }
   }
 
@@ -571,6 +606,8 @@ void prompt_colsum_kernel(SumArgs A) {
   last = __builtin_amdgcn_readfirstlane(last);
   const int t_first = 32 * first / TR, t_end = last < first ? t_first : 32 * last / TR + 1;
 
+  uint32_t q_off[kLoads<4>];
+  row_offsets<4>(q_off, A.qs[2], swz_k);
   f16_t cs[2] = {splat(0.0f), splat(0.0f)};
   float r_lse = 0.0f;
   int2 r_span = make_int2(0, 0);
@@ -579,7 +616,7 @@ void prompt_colsum_kernel(SumArgs A) {
     const uint16_t *rows = qb + g * A.qs[1];
 #pragma unroll
     for (int u = 0; u < TR / 64; ++u)
-      stage_rows<4>(s_rows[buf] + 64 * u * kRowWords, rows, A.qs[2], t * TR + 64 * u, T, swz_k);
+      stage_rows<4>(s_rows[buf] + 64 * u * kRowWords, rows, A.qs[2], t * TR + 64 * u, T, q_off);
     if (tid < TR) {
       const int i = t * TR + tid, ic = min(i, T - 1);
       r_lse = A.lse[((int64_t)b * A.q_heads + kvh * G + g) * T + ic] * kLog2e;
@@ -634,7 +671,7 @@ void prompt_colsum_kernel(SumArgs A) {
               full = full && !__ballot(!(big < A.poly.limit));
             }
             if (full) {
-              Coef c = {0.0f, -lse2, A.scale, A.poly};
+              Coef c = {0.0f, -lse2, A.scale, 0.0f, A.poly};
               if constexpr (BIAS) {
                 c.slope = j0 > i0 ? -slope : slope;
                 c.base = fmaf(c.slope, (float)(j0 + 4 * half - i), c.base);
