@@ -80,6 +80,28 @@ __device__ inline void stage_rows(u4_t *lds, const uint16_t *rows, int64_t strid
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         rsrc, (__attribute__((address_space(3))) void *)(lds + (4 * NW * u + 4 * wave) * kRowWords), 16, off[u], 0, 0, 0);
 }
+// The same through registers: fetch, and keep at the row's place.  The compiler
+// waits for all loads to LDS before any LDS read that could see them, so a kernel
+// whose LDS reads never pause loads its tiles this way, one tile further ahead.
+template <int NW>
+__device__ inline void fetch_rows(u4_t (&w)[kLoads<NW>], const uint16_t *rows, int64_t stride, int row0, int T) {
+  const int lane = threadIdx.x & 63, row = 4 * (threadIdx.x >> 6) + (lane >> 4), have = min(kTileKeys, T - row0);
+  const __amdgpu_buffer_rsrc_t rsrc =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(rows + (int64_t)row0 * stride), (short)0,
+                                        have > 0 ? (int)((have - 1) * stride * 2 + kHeadDim * 2) : 0, 0x00020000);
+#pragma unroll
+  for (int u = 0; u < kLoads<NW>; ++u)
+    w[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (uint32_t)(row + 4 * NW * u) * (uint32_t)(stride * 2) + 16u * (uint32_t)(lane & 15), 0, 0);
+}
+template <int NW, class Swz>
+__device__ inline void keep_rows(u4_t *lds, const u4_t (&w)[kLoads<NW>], Swz swz) {
+  const int lane = threadIdx.x & 63, row = 4 * (threadIdx.x >> 6) + (lane >> 4);
+#pragma unroll
+  for (int u = 0; u < kLoads<NW>; ++u) {
+    const int r = row + 4 * NW * u;
+    lds[r * kRowWords + ((lane & 15) ^ swz(r))] = w[u];
+  }
+}
 // K: 16 lanes read one word of 16 rows; V: 32 lanes read 32 bytes of four rows twice.
 __device__ inline int swz_k(int r) { return r & 15; }
 __device__ inline int swz_v(int r) { return 4 * (r & 3); }
@@ -332,16 +354,21 @@ void prompt_attention_kernel(PromptArgs A) {
     };
 
     const uint32_t off = tile_offset(), voff = v_offset();
-    uint32_t k_off[kLoads<NW>], v_off[kLoads<NW>];
-    row_offsets<NW>(k_off, A.ks[2], swz_k);
-    row_offsets<NW>(v_off, A.vs[2], swz_v);
-    auto load_tile = [&](int t) {
-      stage_rows<NW>(s_k[(t - t_first) & 1], kb, A.ks[2], t * TR, T, k_off);
-      stage_rows<NW>(s_v[(t - t_first) % 3], vb, A.vs[2], t * TR, T, v_off);
+    u4_t rk[kLoads<NW>], rv[kLoads<NW>];
+    auto fetch = [&](int t) {
+      fetch_rows<NW>(rk, kb, A.ks[2], t * TR, T);
+      fetch_rows<NW>(rv, vb, A.vs[2], t * TR, T);
     };
-    load_tile(t_first);
-    if (t_first + 1 < t_end) load_tile(t_first + 1);
-    wait_loads();
+    auto keep = [&](int t) {
+      keep_rows<NW>(s_k[(t - t_first) & 1], rk, swz_k);
+      keep_rows<NW>(s_v[(t - t_first) % 3], rv, swz_v);
+    };
+    // (tiles past the last: their rows are loaded or zeros, and never used)
+    fetch(t_first);
+    keep(t_first);
+    fetch(t_first + 1);
+    keep(t_first + 1);
+    fetch(t_first + 2);
     __syncthreads();
 
     // The subtiles that any query of this wave sees; for the others it only keeps
@@ -350,17 +377,16 @@ void prompt_attention_kernel(PromptArgs A) {
     const int s_last = own_hi > own_lo ? (own_hi + 31) / 32 - 2 * t_first : 0;
     const int n_sub = 2 * (t_end - t_first);
     // The last subtile of a tile: the next tile is complete, and every wave is
-    // done with this tile's keys and the value rows of the one before (turn); then the
-    // tile after the next may be loaded (refill), after this one's LDS reads: the
-    // compiler holds LDS reads back for loads to LDS that are under way.
+    // done with this tile's keys and the value rows of the one before (turn); so the
+    // tile after the next is kept in their place, and the one behind it fetched (refill).
     auto turn = [&](int s) {
-      if (s & 1) {
-        wait_loads();
-        __syncthreads();
-      }
+      if (s & 1) __syncthreads();
     };
     auto refill = [&](int s) {
-      if ((s & 1) && t_first + (s >> 1) + 2 < t_end) load_tile(t_first + (s >> 1) + 2);
+      if (s & 1) {
+        keep(t_first + (s >> 1) + 2);
+        fetch(t_first + (s >> 1) + 3);
+      }
     };
     for (int s = 0; s < s_first; ++s) {
       turn(s);
@@ -415,35 +441,49 @@ void prompt_attention_kernel(PromptArgs A) {
         }
     };
     f16_t d0, d1 = splat(hidden_score<CAP>());
-    bool full1 = false, bad = false;
+    bool full1 = false, bad = false, have_v = true;  // have_v: the value operand is complete
     int j1 = t_first * TR;
     for (int s = s_first; s < s_last; ++s) {
       const int t = s >> 1, j0 = t_first * TR + 32 * s;
       // stage 1: logits of the first query tile, value product of its tile
       // before, weights of the second query tile before
-      float ts;
-      auto none = [](int) {};
-      ts = stage<CAP, BIAS>(d0, kf, bq[0], o[0], vf, p0, d1, coef(full1, 1, j1), p1, none);
+      // (LDS reads are spread over both stages: in one they would take most of its
+      // time from all four waves at once.  The second half of the value rows of
+      // subtile s - 1 comes here, in time for the second half of its product.)
+      const u4_t *vp = s_v[((s - 1) >> 1) % 3] + 32 * ((s - 1) & 1) * kRowWords;
+      auto ahead1 = [&](int i) {
+        if (i < 4 && !have_v) vf[i][1] = read_v(vp, voff, i, 1);
+      };
+      float ts = stage<CAP, BIAS>(d0, kf, bq[0], o[0], vf, p0, d1, coef(full1, 1, j1), p1, ahead1);
       settle(d1, full1, 1, j1, ts, p1);
       if (bad) poison(s - 1, p0, p1);
       const bool full0 = full(0, j0);
       if (!full0) edge(d0, 0, j0);
       turn(s);
       // stage 2: the same for the second query tile, the weights of the first;
-      // the next subtile's keys and this one's value rows are read on the way
+      // the next subtile's keys and half of this one's value rows are read on the way
       const u4_t *kn = s_k[((s + 1) >> 1) & 1], *vn = s_v[t % 3] + 32 * (s & 1) * kRowWords;
       const int kr = 32 * ((s + 1) & 1);
-      auto ahead = [&](int i) {
-        kf[i] = read_word(kn, off, kr, i);
-        vf[i & 3][i >> 2] = read_v(vn, voff, i & 3, i >> 2);
+      auto ahead2 = [&](int i) {
+        if (i < 4) {
+          vf[i][0] = read_v(vn, voff, i, 0);
+        } else {
+          kf[i - 4] = read_word(kn, off, kr, i - 4);
+          kf[i] = read_word(kn, off, kr, i);
+        }
       };
-      ts = stage<CAP, BIAS>(d1, kf, bq[1], o[1], vf, p1, d0, coef(full0, 0, j0), p0, ahead);
+      ts = stage<CAP, BIAS>(d1, kf, bq[1], o[1], vf, p1, d0, coef(full0, 0, j0), p0, ahead2);
       refill(s);
       settle(d0, full0, 0, j0, ts, p0);
       full1 = full(1, j0);
       j1 = j0;
       if (!full1) edge(d1, 1, j0);
-      bad = !(j0 >= seen_lo && j0 + 32 <= seen_hi) && clean();
+      have_v = !(j0 >= seen_lo && j0 + 32 <= seen_hi);
+      if (have_v) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) vf[c][1] = read_v(vn, voff, c, 1);
+      }
+      bad = have_v && clean();
     }
     // the weights of the last second query tile, and both last value products
     {
@@ -461,6 +501,11 @@ void prompt_attention_kernel(PromptArgs A) {
       settle(d1, full1, 1, j1, ts, p1);
       if (bad) poison(s_last - 1, p0, p1);
     }
+    if (!have_v) {
+      const u4_t *vp = s_v[((s_last - 1) >> 1) % 3] + 32 * ((s_last - 1) & 1) * kRowWords;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) vf[c][1] = read_v(vp, voff, c, 1);
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       o[0][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p0[i >> 2]), o[0][i & 3], 0, 0, 0);
@@ -473,7 +518,6 @@ void prompt_attention_kernel(PromptArgs A) {
   }
 
   // out = O / l, through LDS so that whole rows are stored
-  wait_loads();
   __syncthreads();
   u4_t *rows = s_k[0] + wave * (kWaveRows * kRowWords);  // 16 KiB each, s_k and on into s_v
   static_assert(NW <= 2 || sizeof(s_k) == 2 * kWaveRows * kRowWords * 16, "two waves' rows fill s_k");
