@@ -58,46 +58,52 @@ typedef int16_t s4_t __attribute__((ext_vector_type(4)));
 // not overlap).  SWZ(row) is XORed into a row's 16-byte word index; a lane's
 // offsets are the same for every tile.
 template <int NW>
-constexpr int kLoads = kTileKeys / (4 * NW);
+constexpr int tile_loads() { return kTileKeys / (4 * NW); }
+struct RowOffsets {
+  uint32_t at[4];
+};
 template <int NW, class Swz>
-__device__ inline void row_offsets(uint32_t (&off)[kLoads<NW>], int64_t stride, Swz swz) {
+__device__ inline RowOffsets row_offsets(int64_t stride, Swz swz) {
+  static_assert(tile_loads<NW>() <= 4, "offsets of one tile");
+  RowOffsets off;
   const int lane = threadIdx.x & 63, row = 4 * (threadIdx.x >> 6) + (lane >> 4);
 #pragma unroll
-  for (int u = 0; u < kLoads<NW>; ++u) {
+  for (int u = 0; u < tile_loads<NW>(); ++u) {
     const int r = row + 4 * NW * u;
-    off[u] = (uint32_t)r * (uint32_t)(stride * 2) + 16u * (uint32_t)((lane & 15) ^ swz(r));
+    off.at[u] = (uint32_t)r * (uint32_t)(stride * 2) + 16u * (uint32_t)((lane & 15) ^ swz(r));
   }
+  return off;
 }
 template <int NW>
 __device__ inline void stage_rows(u4_t *lds, const uint16_t *rows, int64_t stride, int row0, int T,
-                                  const uint32_t (&off)[kLoads<NW>]) {
+                                  const RowOffsets &off) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), have = min(kTileKeys, T - row0);
   const __amdgpu_buffer_rsrc_t rsrc =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(rows + (int64_t)row0 * stride), (short)0,
                                         have > 0 ? (int)((have - 1) * stride * 2 + kHeadDim * 2) : 0, 0x00020000);
 #pragma unroll
-  for (int u = 0; u < kLoads<NW>; ++u)
+  for (int u = 0; u < tile_loads<NW>(); ++u)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        rsrc, (__attribute__((address_space(3))) void *)(lds + (4 * NW * u + 4 * wave) * kRowWords), 16, off[u], 0, 0, 0);
+        rsrc, (__attribute__((address_space(3))) void *)(lds + (4 * NW * u + 4 * wave) * kRowWords), 16, off.at[u], 0, 0, 0);
 }
 // The same through registers: fetch, and keep at the row's place.  The compiler
 // waits for all loads to LDS before any LDS read that could see them, so a kernel
 // whose LDS reads never pause loads its tiles this way, one tile further ahead.
 template <int NW>
-__device__ inline void fetch_rows(u4_t (&w)[kLoads<NW>], const uint16_t *rows, int64_t stride, int row0, int T) {
+__device__ inline void fetch_rows(u4_t (&w)[tile_loads<NW>()], const uint16_t *rows, int64_t stride, int row0, int T) {
   const int lane = threadIdx.x & 63, row = 4 * (threadIdx.x >> 6) + (lane >> 4), have = min(kTileKeys, T - row0);
   const __amdgpu_buffer_rsrc_t rsrc =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t *>(rows + (int64_t)row0 * stride), (short)0,
                                         have > 0 ? (int)((have - 1) * stride * 2 + kHeadDim * 2) : 0, 0x00020000);
 #pragma unroll
-  for (int u = 0; u < kLoads<NW>; ++u)
+  for (int u = 0; u < tile_loads<NW>(); ++u)
     w[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, (uint32_t)(row + 4 * NW * u) * (uint32_t)(stride * 2) + 16u * (uint32_t)(lane & 15), 0, 0);
 }
 template <int NW, class Swz>
-__device__ inline void keep_rows(u4_t *lds, const u4_t (&w)[kLoads<NW>], Swz swz) {
+__device__ inline void keep_rows(u4_t *lds, const u4_t (&w)[tile_loads<NW>()], Swz swz) {
   const int lane = threadIdx.x & 63, row = 4 * (threadIdx.x >> 6) + (lane >> 4);
 #pragma unroll
-  for (int u = 0; u < kLoads<NW>; ++u) {
+  for (int u = 0; u < tile_loads<NW>(); ++u) {
     const int r = row + 4 * NW * u;
     lds[r * kRowWords + ((lane & 15) ^ swz(r))] = w[u];
   }
@@ -354,7 +360,7 @@ void prompt_attention_kernel(PromptArgs A) {
     };
 
     const uint32_t off = tile_offset(), voff = v_offset();
-    u4_t rk[kLoads<NW>], rv[kLoads<NW>];
+    u4_t rk[tile_loads<NW>()], rv[tile_loads<NW>()];
     auto fetch = [&](int t) {
       fetch_rows<NW>(rk, kb, A.ks[2], t * TR, T);
       fetch_rows<NW>(rv, vb, A.vs[2], t * TR, T);
@@ -650,8 +656,7 @@ void prompt_colsum_kernel(SumArgs A) {
   last = __builtin_amdgcn_readfirstlane(last);
   const int t_first = 32 * first / TR, t_end = last < first ? t_first : 32 * last / TR + 1;
 
-  uint32_t q_off[kLoads<4>];
-  row_offsets<4>(q_off, A.qs[2], swz_k);
+  const RowOffsets q_off = row_offsets<4>(A.qs[2], swz_k);
   f16_t cs[2] = {splat(0.0f), splat(0.0f)};
   float r_lse = 0.0f;
   int2 r_span = make_int2(0, 0);
