@@ -11,17 +11,18 @@
 // that product's reduction is the one they come out in; V^T is read from LDS
 // with the transposing loads in the same order).
 //
-// A wave holds 64 queries (two tiles) of one query head; a block's four waves
-// stream the same K and V rows through LDS.  One wave per SIMD: the output
-// tiles take 128 registers, the queries 64, and every operand read from LDS
-// serves two MFMAs, which halves the LDS traffic that 32 queries per wave would
-// need (all of its bandwidth).  The MFMAs of one half step, the logits of the
-// next tile and the value product of the one before, run beside the
-// exponentials of the tile between them (stage).
+// A wave holds 32 queries of one query head, two waves share a SIMD, and a block's
+// waves stream the same K and V rows through LDS.  Each wave works on three subtiles
+// of 32 keys at once (stage): the logits of one and the value product of another run on
+// the matrix cores beside the weights of the one between.  One wave per SIMD of
+// twice the queries halves the LDS reads, which are 16 % of the time there, but a wave
+// issues an instruction every four to five cycles at best, and a stage has 150 of them
+// beside its sixteen MFMAs of 32 cycles: with two waves they overlap.
 //
 // Every query sees the keys of one interval; a tile that lies inside it for all
 // 32 queries takes the plain path, others are masked first.
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/mikv_layer.h"
 #include "prompt_device.h"
@@ -30,7 +31,11 @@ namespace mikv {
 
 namespace {
 
+// (lambdas with several callers over arrays in registers)
+#define INLINE __attribute__((always_inline))
+
 constexpr int kTileKeys = 64;           // keys per LDS tile
+constexpr int kWaveQueries = 32;        // queries per wave of the attention
 constexpr float kRaise = 1024.0f;       // raise a query's maximum when a lane's 16 weights of a tile sum past this
 constexpr float kInf = __builtin_huge_valf();
 
@@ -165,37 +170,61 @@ __device__ inline uint32_t pack2(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// One half step: the logits `next` = key x query, the value product out += vt x w
-// and, between their MFMAs, the weights `p` of the tile `cur`, whose sum is
-// returned (CAP: infinite where a |d| is past the polynomial's limit).  ahead(i) issues
-// LDS reads after the i-th pair of MFMAs.
+// One half step: the logits `next` = key x query (eight MFMAs, q), the value product
+// out += vt x w (eight, v) and, between them, the weights `p` of the tile `cur`, whose
+// sum is returned (CAP: infinite where a |d| is past the polynomial's limit).
+//   position  0  1  2  3  4  5  6  7  8  9 10 11 12 13 14 15
+//   MFMA      q0 q1 q2 v0 q3 v1 q4 v2 q5 v3 q6 v4 q7 v5 v6 v7
+//   logits    0,1 2,3 4 5 6 7 8 9 10 11 12 13 14 15  -  -
+// The logits end three MFMAs before the half step does, so that the next one's
+// first weights need not wait for them, and the weights two before it, so that their
+// sum is there when it ends.  ahead(k) issues LDS operations at position k.
 template <bool CAP, bool BIAS, class Ahead>
 __device__ inline float stage(f16_t &next, const u4_t (&key)[8], const u4_t (&query)[8], f16_t (&out)[4],
                               u4_t (&vt)[4][2], const u4_t (&w)[2], const f16_t &cur, const Coef &c, u4_t (&p)[2],
                               Ahead ahead) {
   f16_t d = splat(0.0f);
-  float ts[2] = {0.0f, 0.0f}, big = 0.0f;
-  float x0 = term<CAP, BIAS>(cur[0], 0, c), x1 = term<CAP, BIAS>(cur[1], 1, c);
+  float ts[2] = {0.0f, 0.0f}, big = 0.0f, x[2], e[2];
+  x[0] = term<CAP, BIAS>(cur[0], 0, c);
+  x[1] = term<CAP, BIAS>(cur[1], 1, c);
+  int q = 0, v = 0, r = 0;  // constants once unrolled
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    d = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(key[i]), as_h8(query[i]), d, 0, 0, 0);
-    out[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vt[i & 3][i >> 2]), as_h8(w[i >> 2]), out[i & 3], 0, 0, 0);
-    ahead(i);
-    float p0 = __builtin_amdgcn_exp2f(x0), p1 = __builtin_amdgcn_exp2f(x1);
-    if (i < 7) {
-      x0 = term<CAP, BIAS>(cur[2 * i + 2], 2 * i + 2, c);
-      x1 = term<CAP, BIAS>(cur[2 * i + 3], 2 * i + 3, c);
+  for (int k = 0; k < 16; ++k) {
+    if (k < 3 || (k < 13 && k % 2 == 0)) {
+      d = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(key[q]), as_h8(query[q]), d, 0, 0, 0);
+      ++q;
+    } else {
+      out[v & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vt[v & 3][v >> 2]), as_h8(w[v >> 2]), out[v & 3], 0, 0, 0);
+      ++v;
     }
-    ts[0] += p0;
-    ts[1] += p1;
-    uint32_t w2 = pack2(p0, p1);
-    if constexpr (CAP) big = fmaxf(big, fmaxf(fabsf(cur[2 * i]), fabsf(cur[2 * i + 1])));
-    asm volatile("" : "+v"(w2), "+v"(ts[0]), "+v"(ts[1]), "+v"(big));  // here: the compiler would move all this behind the MFMAs
-    p[i >> 2][i & 3] = w2;
+    ahead(k);
+    const int n = k < 2 ? 2 : k < 14 ? 1 : 0;
+#pragma unroll
+    for (int h = 0; h < n; ++h, ++r) {
+      float pr = __builtin_amdgcn_exp2f(x[r & 1]);
+      if constexpr (CAP) big = fmaxf(big, fabsf(cur[r]));
+      if (r < 14) x[r & 1] = term<CAP, BIAS>(cur[r + 2], r + 2, c);
+      ts[r & 1] += pr;
+      // (here: the compiler would move all this behind the MFMAs)
+      if (r & 1) {
+        uint32_t w2 = pack2(e[0], pr);
+        asm volatile("" : "+v"(w2), "+v"(ts[0]), "+v"(ts[1]), "+v"(big));
+        p[r >> 3][(r >> 1) & 3] = w2;
+      } else {
+        asm volatile("" : "+v"(pr));
+        e[0] = pr;
+      }
+    }
     __builtin_amdgcn_sched_barrier(0);
   }
   next = d;
   return CAP && !(big < c.limit) ? kInf : ts[0] + ts[1];
+}
+
+// The value of the lane 32 away (no LDS operation, which would be in the way of the loop's own).
+__device__ inline float other_half(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
 }
 
 __device__ inline int wave_min_int(int v) {
@@ -215,53 +244,45 @@ __device__ inline void query_span(const int32_t *begin, const int32_t *end, int 
 }
 
 // A block of NW waves: min(G, NW) query heads of one KV head's group times the
-// 64-query tiles that fill it, so that its waves need the same keys as nearly as
+// 32-query tiles that fill it, so that its waves need the same keys as nearly as
 // they can.
 template <bool CAP, bool BIAS, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(1, 1)))
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void prompt_attention_kernel(PromptArgs A) {
-  constexpr int TR = kTileKeys;
-  __shared__ u4_t s_k[2][TR * kRowWords];
-  __shared__ u4_t s_v[3][TR * kRowWords];
-  int(*s_span)[2] = reinterpret_cast<int(*)[2]>(s_v[2]);  // free until the third tile
+  constexpr int TR = kTileKeys, kTile = TR * kRowWords;
+  __shared__ u4_t s_lds[5 * kTile];  // three tiles of K, two of V
+  auto k_tile = [&](int t) INLINE { return s_lds + (t % 3) * kTile; };
+  auto v_tile = [&](int t) INLINE { return s_lds + (3 + (t & 1)) * kTile; };
+  int(*s_span)[2] = reinterpret_cast<int(*)[2]>(s_lds + 2 * kTile);  // free until the third tile
   const int lane = threadIdx.x & 63, n = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int G = A.q_heads / A.kv_heads, T = A.T;
-  const int hw = min(G, NW), rw = NW / hw, groups = G / hw;  // heads and row tiles of a block, head groups
+  const int hw = min(G, NW), rw = NW / hw, groups = G / hw;  // heads and query tiles of a block, head groups
   int hk, idx;
   if (!block_unit(A.units, A.nblk * groups, A.run, hk, idx)) return;
   const int b = hk / A.kv_heads, kvh = hk % A.kv_heads, head = kvh * G + (idx % groups) * hw + wave % hw;
-  const int i_wave = kWaveRows * ((A.nblk - 1 - idx / groups) * rw + wave / hw);
+  const int i_wave = kWaveQueries * ((A.nblk - 1 - idx / groups) * rw + wave / hw);
   const uint16_t *kb = A.k + b * A.ks[0] + kvh * A.ks[1], *vb = A.v + b * A.vs[0] + kvh * A.vs[1];
   const uint16_t *qb = A.q + b * A.qs[0] + head * A.qs[1];
 
   // The queries, and their intervals (queries past the prompt repeat the last one).
-  u4_t bq[2][8];
-  int lo[2], hi[2], i_own[2], full_lo[2], full_hi[2];
-  int any_lo = T, any_hi = 0;
+  const int i_own = min(i_wave + n, T - 1), i_lo = min(i_wave, T - 1), i_hi = min(i_wave + 31, T - 1);
+  u4_t bq[8];
+  {
+    const uint16_t *r = qb + (int64_t)i_own * A.qs[2] + 8 * half;
 #pragma unroll
-  for (int cb = 0; cb < 2; ++cb) {
-    const int i = min(i_wave + 32 * cb + n, T - 1);
-    i_own[cb] = i;
-    const uint16_t *r = qb + (int64_t)i * A.qs[2] + 8 * half;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) bq[cb][c] = *reinterpret_cast<const u4_t *>(r + 16 * c);
-    // in the accumulation registers, from which the MFMAs read them (the others
-    // are full; without this they are copied back for every use)
-#pragma unroll
-    for (int c = 0; c < 8; ++c) asm volatile("" : "+a"(bq[cb][c]));
-    query_span(A.begin, A.end, A.window, (int64_t)b * T + i, i, T, lo[cb], hi[cb]);
-    full_lo[cb] = wave_max_int(lo[cb]);
-    full_hi[cb] = wave_min_int(hi[cb]);
-    any_lo = min(any_lo, wave_min_int(hi[cb] ? lo[cb] : T));
-    any_hi = max(any_hi, wave_max_int(hi[cb]));
+    for (int c = 0; c < 8; ++c) bq[c] = *reinterpret_cast<const u4_t *>(r + 16 * c);
   }
-  const int own_lo = any_lo, own_hi = any_hi;
+  int lo, hi;
+  query_span(A.begin, A.end, A.window, (int64_t)b * T + i_own, i_own, T, lo, hi);
+  const int full_lo = wave_max_int(lo), full_hi = wave_min_int(hi);
+  const int own_lo = wave_min_int(hi ? lo : T), own_hi = wave_max_int(hi);
   if (lane == 0) {
-    s_span[wave][0] = any_lo;
-    s_span[wave][1] = any_hi;
+    s_span[wave][0] = own_lo;
+    s_span[wave][1] = own_hi;
   }
   __syncthreads();
+  int any_lo = own_lo, any_hi = own_hi;
 #pragma unroll
   for (int w = 0; w < NW; ++w) {
     any_lo = min(any_lo, s_span[w][0]);
@@ -269,30 +290,25 @@ void prompt_attention_kernel(PromptArgs A) {
   }
   any_lo = __builtin_amdgcn_readfirstlane(any_lo);
   any_hi = __builtin_amdgcn_readfirstlane(any_hi);
-  const int t_first = any_lo / TR, t_end = max(t_first, (any_hi + TR - 1) / TR);
+  const int t_first = any_lo / TR, n_tiles = max(0, (any_hi + TR - 1) / TR - t_first);
 
   const float slope = BIAS ? A.slopes[head] * kLog2e : 0.0f;
-  float m[2] = {-kInf, -kInf}, l[2] = {0.0f, 0.0f};
-  f16_t o[2][4];
+  float m = -kInf, l = 0.0f;
+  f16_t o[4];
 #pragma unroll
-  for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-    for (int c = 0; c < 4; ++c) o[cb][c] = splat(0.0f);
+  for (int c = 0; c < 4; ++c) o[c] = splat(0.0f);
 
-  if (t_first < t_end) {
-    const int seen_lo = max(full_lo[0], full_lo[1]), seen_hi = min(full_hi[0], full_hi[1]);  // by every query of the wave
-    const int i_lo[2] = {min(i_wave, T - 1), min(i_wave + 32, T - 1)};
-    const int i_hi[2] = {min(i_wave + 31, T - 1), min(i_wave + 63, T - 1)};
-    // whether every query of tile cb sees keys j0 .. j0 + 31, on one side of it where the bias needs that
-    auto full = [&](int cb, int j0) {
-      bool f = j0 >= full_lo[cb] && j0 + 32 <= full_hi[cb];
-      if constexpr (BIAS) f = f && (j0 + 31 <= i_lo[cb] || j0 > i_hi[cb]);
+  if (n_tiles > 0) {
+    // whether every query sees keys j0 .. j0 + 31, on one side of it where the bias needs that
+    auto full = [&](int j0) INLINE {
+      bool f = j0 >= full_lo && j0 + 32 <= full_hi;
+      if constexpr (BIAS) f = f && (j0 + 31 <= i_lo || j0 > i_hi);
       return f;
     };
-    auto coef = [&](bool is_full, int cb, int j0) {
+    auto coef = [&](bool is_full, int j0) INLINE {
       Coef c;
       c.slope = 0.0f;
-      c.base = -m[cb];
+      c.base = -m;
       if constexpr (CAP) {
         c.p.c0 = is_full ? A.poly.c0 : 1.0f;
         c.p.c1 = is_full ? A.poly.c1 : 0.0f;
@@ -304,114 +320,111 @@ void prompt_attention_kernel(PromptArgs A) {
         c.scale = is_full ? A.scale : 1.0f;
       }
       if constexpr (BIAS) {
-        c.slope = !is_full ? 0.0f : j0 > i_hi[cb] ? -slope : slope;
-        c.base = fmaf(c.slope, (float)(j0 + 4 * half - i_own[cb]), c.base);
+        c.slope = !is_full ? 0.0f : j0 > i_hi ? -slope : slope;
+        c.base = fmaf(c.slope, (float)(j0 + 4 * half - i_own), c.base);
       }
       return c;
     };
-    // final scores of a tile of which not every query sees every key
-    auto edge = [&](f16_t &d, int cb, int j0) {
+    // final scores of a subtile of which not every query sees every key
+    auto edge = [&](f16_t &d, int j0) INLINE {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = j0 + tile_row(r);
         float s = CAP ? tanh_fine(d[r] * A.scale) * A.cap : d[r] * A.scale;
-        if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own[cb] - j), s);
+        if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own - j), s);
         if constexpr (CAP) s = s < kLowest ? kLowest : s;
-        d[r] = j >= lo[cb] && j < hi[cb] ? s : hidden_score<CAP>();
+        d[r] = j >= lo && j < hi ? s : hidden_score<CAP>();
       }
     };
-    // Where a tile's weights sum past kRaise (or are NaN: the maximum starts at
+    // Whether every lane's weights of a subtile are in range.
+    auto fine = [&](float ts) INLINE { return __ballot(!(ts <= kRaise)) == 0; };
+    // Where a subtile's weights sum past kRaise (or are NaN: the maximum starts at
     // -inf; or not valid, see stage) in any lane: raise the maxima, rescale, and
-    // weigh the tile again.  The two lanes of a query keep one maximum.
-    auto settle = [&](const f16_t &d, bool is_full, int cb, int j0, float ts, u4_t (&p)[2]) {
-      if (__ballot(!(ts <= kRaise))) {
-        Coef c = coef(is_full, cb, j0);
-        c.base = BIAS ? c.slope * (float)(j0 + 4 * half - i_own[cb]) : 0.0f;
-        float s[16], mx = -kInf;
+    // weigh the subtile again.  The two lanes of a query keep one maximum.
+    auto raise = [&](const f16_t &d, bool is_full, int j0, float &ts, u4_t (&p)[2]) INLINE {
+      Coef c = coef(is_full, j0);
+      c.base = BIAS ? c.slope * (float)(j0 + 4 * half - i_own) : 0.0f;
+      float s[16], mx = -kInf;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if constexpr (CAP) {
-            s[r] = is_full ? fmaf(tanh_fine(d[r] * A.scale), A.cap, BIAS ? fmaf(c.slope, row_const(r), c.base) : 0.0f)
-                           : d[r] < 5.0f * kLowest ? -kInf : d[r];
-          } else {
-            s[r] = term<CAP, BIAS>(d[r], r, c);
-          }
-          mx = fmaxf(mx, s[r]);
+      for (int r = 0; r < 16; ++r) {
+        if constexpr (CAP) {
+          s[r] = is_full ? fmaf(tanh_fine(d[r] * A.scale), A.cap, BIAS ? fmaf(c.slope, row_const(r), c.base) : 0.0f)
+                         : d[r] < 5.0f * kLowest ? -kInf : d[r];
+        } else {
+          s[r] = term<CAP, BIAS>(d[r], r, c);
         }
-        mx = fmaxf(m[cb], fmaxf(mx, __shfl_xor(mx, 32, 64)));
-        const float ref = mx == -kInf ? 0.0f : mx;
-        const float f = m[cb] == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m[cb] - ref);
-        m[cb] = mx;
-        l[cb] *= f;
-#pragma unroll
-        for (int c4 = 0; c4 < 4; ++c4)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[cb][c4][r] *= f;
-        ts = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[r] = __builtin_amdgcn_exp2f(s[r] - ref);
-          ts += s[r];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = pack2(s[2 * i], s[2 * i + 1]);
+        mx = fmaxf(mx, s[r]);
       }
-      l[cb] += ts;
+      mx = fmaxf(m, fmaxf(mx, other_half(mx)));
+      const float ref = mx == -kInf ? 0.0f : mx;
+      const float f = m == -kInf ? 0.0f : __builtin_amdgcn_exp2f(m - ref);
+      m = mx;
+      l *= f;
+#pragma unroll
+      for (int c4 = 0; c4 < 4; ++c4)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c4][r] *= f;
+      ts = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(s[r] - ref);
+        ts += s[r];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = pack2(s[2 * i], s[2 * i + 1]);
+      return f;
     };
+
+    // The tiles pass through registers, K and V in turn: tile t + 1's keys are kept in
+    // LDS during the first subtile of tile t, its value rows during the second, each
+    // fetched one subtile before.  (Past the last tile rows are loaded, or zeros,
+    // and never used.)
+    u4_t rows[tile_loads<NW>()];
+    auto fetch_keys = [&](int t) INLINE { fetch_rows<NW>(rows, kb, A.ks[2], (t_first + t) * TR, T); };
+    auto fetch_values = [&](int t) INLINE { fetch_rows<NW>(rows, vb, A.vs[2], (t_first + t) * TR, T); };
+    auto feed_keys = [&](int t) INLINE {
+      keep_rows<NW>(k_tile(t), rows, swz_k);
+      fetch_values(t);
+    };
+    auto feed_values = [&](int t) INLINE {
+      keep_rows<NW>(v_tile(t), rows, swz_v);
+      fetch_keys(t + 1);
+    };
+    fetch_keys(0);
+    feed_keys(0);
+    feed_values(0);
+    __syncthreads();
+    // A tile that this wave does not see.  At the barrier the next tile's keys and
+    // this one's value rows are complete, and every wave is done with the keys of the tile
+    // before and with its value rows.
+    auto idle = [&](int t) INLINE {
+      feed_keys(t + 1);
+      __syncthreads();
+      feed_values(t + 1);
+    };
+
+    // The tiles that any query of this wave sees; for the others it only keeps step
+    // with the block.
+    const int own_first = own_hi > own_lo ? own_lo / TR - t_first : 0;
+    const int own_end = own_hi > own_lo ? (own_hi + TR - 1) / TR - t_first : 0;
+    for (int t = 0; t < own_first; ++t) idle(t);
 
     const uint32_t off = tile_offset(), voff = v_offset();
-    u4_t rk[tile_loads<NW>()], rv[tile_loads<NW>()];
-    auto fetch = [&](int t) {
-      fetch_rows<NW>(rk, kb, A.ks[2], t * TR, T);
-      fetch_rows<NW>(rv, vb, A.vs[2], t * TR, T);
-    };
-    auto keep = [&](int t) {
-      keep_rows<NW>(s_k[(t - t_first) & 1], rk, swz_k);
-      keep_rows<NW>(s_v[(t - t_first) % 3], rv, swz_v);
-    };
-    // (tiles past the last: their rows are loaded or zeros, and never used)
-    fetch(t_first);
-    keep(t_first);
-    fetch(t_first + 1);
-    keep(t_first + 1);
-    fetch(t_first + 2);
-    __syncthreads();
-
-    // The subtiles that any query of this wave sees; for the others it only keeps
-    // step with the block.
-    const int s_first = own_hi > own_lo ? own_lo / 32 - 2 * t_first : 0;
-    const int s_last = own_hi > own_lo ? (own_hi + 31) / 32 - 2 * t_first : 0;
-    const int n_sub = 2 * (t_end - t_first);
-    // The last subtile of a tile: the next tile is complete, and every wave is
-    // done with this tile's keys and the value rows of the one before (turn); so the
-    // tile after the next is kept in their place, and the one behind it fetched (refill).
-    auto turn = [&](int s) {
-      if (s & 1) __syncthreads();
-    };
-    auto refill = [&](int s) {
-      if (s & 1) {
-        keep(t_first + (s >> 1) + 2);
-        fetch(t_first + (s >> 1) + 3);
-      }
-    };
-    for (int s = 0; s < s_first; ++s) {
-      turn(s);
-      refill(s);
-    }
-    // Before the first subtile: weights and value operands of zero, and a second
-    // tile that sees nothing (edge form), with its first key.
+    // Before the first subtile: weights and value operands of zero, and a subtile
+    // that sees nothing (edge form).
     u4_t kf[8], vf[4][2], p0[2], p1[2];
 #pragma unroll
     for (int i = 0; i < 8; ++i) vf[i & 3][i >> 2] = u4_t{0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 2; ++i) p0[i] = p1[i] = u4_t{0, 0, 0, 0};
-    read_tile(s_k[(s_first >> 1) & 1], off, 32 * (s_first & 1), kf);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) kf[i] = read_word(k_tile(own_first), off, 0, i);
     // A value of a row that some query does not see must not reach that query as
     // 0 x NaN: in an edge subtile infinities and NaN are taken out of the value
     // operand (clean says whether any were there), and the queries that do see
-    // one become NaN in its channel (poison, once the subtile's weights are known).
-    auto odd_halves = [](uint32_t w) { return (((w & 0x7fff7fffu) + 0x04000400u) & 0x80008000u) >> 15; };  // 1 per infinite or NaN half
-    auto clean = [&]() {
+    // one become NaN in its channel (poison).
+    auto odd_halves = [](uint32_t w) INLINE { return (((w & 0x7fff7fffu) + 0x04000400u) & 0x80008000u) >> 15; };  // 1 per infinite or NaN half
+    auto clean = [&]() INLINE {
       uint32_t any = 0u;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -424,135 +437,129 @@ void prompt_attention_kernel(PromptArgs A) {
         for (int e = 0; e < 4; ++e) vf[i & 3][i >> 2][e] &= ~(odd_halves(vf[i & 3][i >> 2][e]) * 0xffffu);
       return true;
     };
-    auto poison = [&](int s, const u4_t (&w0)[2], const u4_t (&w1)[2]) {
-      const u4_t *v = s_v[(s >> 1) % 3] + 32 * (s & 1) * kRowWords;
-      auto ones = [](uint32_t w) { return ((w & 0xffffu) ? 0x3c00u : 0u) | ((w >> 16) ? 0x3c000000u : 0u); };
+    auto poison = [&](const u4_t *v, const u4_t (&p)[2]) INLINE {
+      auto ones = [](uint32_t w) INLINE { return ((w & 0xffffu) ? 0x3c00u : 0u) | ((w >> 16) ? 0x3c000000u : 0u); };
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < 4; ++c) {
+        f16_t hits = splat(0.0f);
 #pragma unroll
-        for (int cb = 0; cb < 2; ++cb) {
-          f16_t hits = splat(0.0f);
+        for (int kh = 0; kh < 2; ++kh) {
+          u4_t a = read_v(v, voff, c, kh), w = p[kh];
 #pragma unroll
-          for (int kh = 0; kh < 2; ++kh) {
-            u4_t a = read_v(v, voff, c, kh), w = cb ? w1[kh] : w0[kh];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              a[e] = odd_halves(a[e]) * 0x3c00u;
-              w[e] = ones(w[e]);
-            }
-            hits = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(a), as_h8(w), hits, 0, 0, 0);
+          for (int e = 0; e < 4; ++e) {
+            a[e] = odd_halves(a[e]) * 0x3c00u;
+            w[e] = ones(w[e]);
           }
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[cb][c][r] += hits[r] > 0.0f ? __builtin_nanf("") : 0.0f;
+          hits = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(a), as_h8(w), hits, 0, 0, 0);
         }
-    };
-    f16_t d0, d1 = splat(hidden_score<CAP>());
-    bool full1 = false, bad = false, have_v = true;  // have_v: the value operand is complete
-    int j1 = t_first * TR;
-    for (int s = s_first; s < s_last; ++s) {
-      const int t = s >> 1, j0 = t_first * TR + 32 * s;
-      // stage 1: logits of the first query tile, value product of its tile
-      // before, weights of the second query tile before
-      // (LDS reads are spread over both stages: in one they would take most of its
-      // time from all four waves at once.  The second half of the value rows of
-      // subtile s - 1 comes here, in time for the second half of its product.)
-      const u4_t *vp = s_v[((s - 1) >> 1) % 3] + 32 * ((s - 1) & 1) * kRowWords;
-      auto ahead1 = [&](int i) {
-        if (i < 4 && !have_v) vf[i][1] = read_v(vp, voff, i, 1);
-      };
-      float ts = stage<CAP, BIAS>(d0, kf, bq[0], o[0], vf, p0, d1, coef(full1, 1, j1), p1, ahead1);
-      settle(d1, full1, 1, j1, ts, p1);
-      if (bad) poison(s - 1, p0, p1);
-      const bool full0 = full(0, j0);
-      if (!full0) edge(d0, 0, j0);
-      turn(s);
-      // stage 2: the same for the second query tile, the weights of the first;
-      // the next subtile's keys and half of this one's value rows are read on the way
-      const u4_t *kn = s_k[((s + 1) >> 1) & 1], *vn = s_v[t % 3] + 32 * (s & 1) * kRowWords;
-      const int kr = 32 * ((s + 1) & 1);
-      auto ahead2 = [&](int i) {
-        if (i < 4) {
-          vf[i][0] = read_v(vn, voff, i, 0);
-        } else {
-          kf[i - 4] = read_word(kn, off, kr, i - 4);
-          kf[i] = read_word(kn, off, kr, i);
-        }
-      };
-      ts = stage<CAP, BIAS>(d1, kf, bq[1], o[1], vf, p1, d0, coef(full0, 0, j0), p0, ahead2);
-      refill(s);
-      settle(d0, full0, 0, j0, ts, p0);
-      full1 = full(1, j0);
-      j1 = j0;
-      if (!full1) edge(d1, 1, j0);
-      have_v = !(j0 >= seen_lo && j0 + 32 <= seen_hi);
-      if (have_v) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) vf[c][1] = read_v(vn, voff, c, 1);
+        for (int r = 0; r < 16; ++r) o[c][r] += hits[r] > 0.0f ? __builtin_nanf("") : 0.0f;
       }
-      bad = have_v && clean();
+    };
+    f16_t d0 = splat(hidden_score<CAP>()), d1;
+    bool was_full = false;  // of the subtile before
+    // Its first key and value rows.  Before the first subtile: rows that are complete
+    // (those of the first tile come after the barrier), with weights of zero; infinities
+    // and NaN are taken out of them unless every query sees them anyway.
+    const int t_zero = max(own_first - 1, 0);
+    int j_was = (t_first + t_zero) * TR;
+    const u4_t *v_was = v_tile(t_zero);
+    // One subtile: logits of it into `d`, weights of the one before, whose logits `was`
+    // holds, into `p`, and value product of the one before that, whose weights `pv` holds.
+    auto subtile = [&](auto which, int t, f16_t &d, f16_t &was, u4_t (&p)[2], u4_t (&pv)[2]) INLINE {
+      constexpr int S = decltype(which)::value;  // of the tile's two
+      const int j0 = (t_first + t) * TR + 32 * S;
+      if constexpr (S == 1) __syncthreads();
+      const u4_t *kt = k_tile(t), *kn = k_tile(t + S);
+      auto ahead = [&](int k) INLINE {
+        // this subtile's second half of the keys, the value rows of the subtile before
+        // and the next one's first half of the keys, in time for their MFMAs and as the
+        // operands they take the place of are done with
+        if (k < 4) kf[4 + k] = read_word(kt, off, 32 * S, 4 + k);
+        if (k >= 4 && k <= 10 && k % 2 == 0) vf[(k - 4) / 2][0] = read_v(v_was, voff, (k - 4) / 2, 0);
+        if (k == 5) {
+          if constexpr (S == 0)
+            feed_keys(t + 1);
+          else
+            feed_values(t + 1);
+        }
+        if (k >= 11 && k <= 14) kf[k - 11] = read_word(kn, off, 32 * (1 - S), k - 11);
+      };
+      float ts = stage<CAP, BIAS>(d, kf, bq, o, vf, pv, was, coef(was_full, j_was), p, ahead);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) vf[c][1] = read_v(v_was, voff, c, 1);
+      const bool is_full = full(j0), ok = fine(ts);
+      // (one branch, rarely taken, for all that is not plain)
+      if (__builtin_expect(!ok || !is_full || !was_full, false)) {
+        if (!ok) raise(was, was_full, j_was, ts, p);
+        if (!is_full) edge(d, j0);
+        if (!(j_was >= full_lo && j_was + 32 <= full_hi) && clean()) poison(v_was, p);
+      }
+      l += ts;
+      was_full = is_full;
+      j_was = j0;
+      v_was = v_tile(t) + 32 * S * kRowWords;
+    };
+    for (int t = own_first; t < own_end; ++t) {
+      subtile(std::integral_constant<int, 0>{}, t, d1, d0, p0, p1);
+      subtile(std::integral_constant<int, 1>{}, t, d0, d1, p1, p0);
     }
-    // the weights of the last second query tile, and both last value products
+    // the weights of the last subtile, and both last value products
+    auto product = [&](const u4_t (&p)[2]) INLINE {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p[i >> 2]), o[i & 3], 0, 0, 0);
+    };
+    product(p1);
     {
-      const Coef c = coef(full1, 1, j1);
+      const Coef c = coef(was_full, j_was);
       float ts = 0.0f, big = 0.0f, x[16];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        x[r] = __builtin_amdgcn_exp2f(term<CAP, BIAS>(d1[r], r, c));
+        x[r] = __builtin_amdgcn_exp2f(term<CAP, BIAS>(d0[r], r, c));
         ts += x[r];
-        big = fmaxf(big, fabsf(d1[r]));
+        big = fmaxf(big, fabsf(d0[r]));
       }
       if (CAP && !(big < c.limit)) ts = kInf;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p1[i >> 2][i & 3] = pack2(x[2 * i], x[2 * i + 1]);
-      settle(d1, full1, 1, j1, ts, p1);
-      if (bad) poison(s_last - 1, p0, p1);
+      for (int i = 0; i < 8; ++i) p0[i >> 2][i & 3] = pack2(x[2 * i], x[2 * i + 1]);
+      if (!fine(ts)) raise(d0, was_full, j_was, ts, p0);
+      l += ts;
     }
-    if (!have_v) {
-      const u4_t *vp = s_v[((s_last - 1) >> 1) % 3] + 32 * ((s_last - 1) & 1) * kRowWords;
+    if (own_first < own_end) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) vf[c][1] = read_v(vp, voff, c, 1);
+      for (int i = 0; i < 8; ++i) vf[i & 3][i >> 2] = read_v(v_was, voff, i & 3, i >> 2);
+      if (!(j_was >= full_lo && j_was + 32 <= full_hi) && clean()) poison(v_was, p0);
+      product(p0);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      o[0][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p0[i >> 2]), o[0][i & 3], 0, 0, 0);
-      o[1][i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_f16(as_h8(vf[i & 3][i >> 2]), as_h8(p1[i >> 2]), o[1][i & 3], 0, 0, 0);
-    }
-    for (int s = s_last; s < n_sub; ++s) {
-      turn(s);
-      refill(s);
-    }
+    for (int t = own_end; t < n_tiles; ++t) idle(t);
   }
 
   // out = O / l, through LDS so that whole rows are stored
   __syncthreads();
-  u4_t *rows = s_k[0] + wave * (kWaveRows * kRowWords);  // 16 KiB each, s_k and on into s_v
-  static_assert(NW <= 2 || sizeof(s_k) == 2 * kWaveRows * kRowWords * 16, "two waves' rows fill s_k");
-  if (NW > 2 && wave >= 2) rows = s_v[wave - 2];
+  u4_t *own_rows = s_lds + wave * (kWaveQueries * kRowWords);  // 8 KiB each
+  const float sum = l + other_half(l);
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  if (A.lse && half == 0 && i_wave + n < T)
+    A.lse[((int64_t)b * A.q_heads + head) * T + i_wave + n] =
+        sum == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+  uint2 *row = reinterpret_cast<uint2 *>(own_rows) + n * (2 * kRowWords);
 #pragma unroll
-  for (int cb = 0; cb < 2; ++cb) {
-    const float sum = l[cb] + __shfl_xor(l[cb], 32, 64);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int i = i_wave + 32 * cb + n;
-    if (A.lse && half == 0 && i < T)
-      A.lse[((int64_t)b * A.q_heads + head) * T + i] = sum == 0.0f ? -kInf : (m[cb] + __builtin_amdgcn_logf(sum)) * kLn2;
-    uint2 *row = reinterpret_cast<uint2 *>(rows) + (32 * cb + n) * (2 * kRowWords);
+  for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const int w = 4 * c + a;  // 16-byte word: channels 32 c + 8 a ..
-        row[2 * (w ^ (n & 15)) + half] = make_uint2(pack2(o[cb][c][4 * a] * inv, o[cb][c][4 * a + 1] * inv),
-                                                   pack2(o[cb][c][4 * a + 2] * inv, o[cb][c][4 * a + 3] * inv));
-      }
-  }
+    for (int a = 0; a < 4; ++a) {
+      const int w = 4 * c + a;  // 16-byte word: channels 32 c + 8 a ..
+      row[2 * (w ^ (n & 15)) + half] = make_uint2(pack2(o[c][4 * a] * inv, o[c][4 * a + 1] * inv),
+                                                 pack2(o[c][4 * a + 2] * inv, o[c][4 * a + 3] * inv));
+    }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
   uint16_t *ob = A.out + b * A.os[0] + head * A.os[1];
 #pragma unroll
-  for (int u = 0; u < 16; ++u) {
+  for (int u = 0; u < kWaveQueries / 4; ++u) {
     const int r = 4 * u + (lane >> 4), i = i_wave + r;
-    const u4_t w = rows[r * kRowWords + ((lane & 15) ^ (r & 15))];
+    const u4_t w = own_rows[r * kRowWords + ((lane & 15) ^ (r & 15))];
     if (i < T) *reinterpret_cast<u4_t *>(ob + (int64_t)i * A.os[2] + 8 * (lane & 15)) = w;
   }
 }
@@ -827,7 +834,7 @@ void copy3(T d[3], const T s[3]) { d[0] = s[0], d[1] = s[1], d[2] = s[2]; }
 
 template <int NW>
 void launch_attention(PromptArgs &A, int G, bool cap, bool bias, hipStream_t st) {
-  const int hw = std::min(G, NW), rows = kWaveRows * (NW / hw), per_unit = (A.T + rows - 1) / rows * (G / hw);
+  const int hw = std::min(G, NW), rows = kWaveQueries * (NW / hw), per_unit = (A.T + rows - 1) / rows * (G / hw);
   A.nblk = (A.T + rows - 1) / rows;
   A.run = (int)std::min<int64_t>((int64_t)A.units * per_unit >= 4096 ? 32 : 4, per_unit);
   const dim3 grid(grid_blocks(A.units, per_unit, A.run));
@@ -867,7 +874,7 @@ extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rule
   const int G = p->q_heads / p->kv_heads;
   score_scales(p->scale, rules ? rules->cap : 0.0f, A);
   const bool cap = A.cap > 0.0f, bias = A.slopes != nullptr;
-  launch_attention<4>(A, G, cap, bias, (hipStream_t)stream);
+  launch_attention<8>(A, G, cap, bias, (hipStream_t)stream);
   return check_launch(who);
 }
 
