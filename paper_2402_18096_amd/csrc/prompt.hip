@@ -477,7 +477,7 @@ void prompt_attention_kernel(PromptArgs A) {
         // operands they take the place of are done with
         if (k < 4) kf[4 + k] = read_word(kt, off, 32 * S, 4 + k);
         if (k >= 4 && k <= 10 && k % 2 == 0) vf[(k - 4) / 2][0] = read_v(v_was, voff, (k - 4) / 2, 0);
-        if (k == 5) {
+        if (k == 2) {
           if constexpr (S == 0)
             feed_keys(t + 1);
           else
@@ -699,8 +699,6 @@ void prompt_colsum_kernel(SumArgs A) {
     for (int g = 0; g < G; ++g) {
       const float slope = BIAS ? A.slopes[kvh * G + g] * kLog2e : 0.0f;
       for (int t = t_first; t < t_end; ++t) {
-        const bool wrap = t + 1 == t_end;
-        load(buf ^ 1, wrap ? min(g + 1, G - 1) : g, wrap ? t_first : t + 1);
         const u4_t *rows = s_rows[buf];
 #pragma unroll
         for (int s = 0; s < SUBS; ++s) {
@@ -708,11 +706,15 @@ void prompt_colsum_kernel(SumArgs A) {
           const int4 sp = s_sub[buf][sub];
           const int any_lo = __builtin_amdgcn_readfirstlane(sp.x), any_hi = __builtin_amdgcn_readfirstlane(sp.y);
           const int full_lo = __builtin_amdgcn_readfirstlane(sp.z), full_hi = __builtin_amdgcn_readfirstlane(sp.w);
-          if (any_lo >= j_wave + kWaveRows || any_hi <= j_wave) continue;  // wave-uniform
           u4_t bq[8];
           read_tile(rows, off, 32 * sub, bq);
           const float lse2 = s_lse[buf][32 * sub + n];
           const int2 span = s_span[buf][32 * sub + n];
+          if (s == SUBS - 1) {  // after the tile's last LDS read: the compiler holds LDS reads back for loads to LDS
+            const bool wrap = t + 1 == t_end;
+            load(buf ^ 1, wrap ? min(g + 1, G - 1) : g, wrap ? t_first : t + 1);
+          }
+          if (any_lo >= j_wave + kWaveRows || any_hi <= j_wave) continue;  // wave-uniform
           const int i = min(i0 + n, T - 1);
 #pragma unroll
           for (int cb = 0; cb < 2; ++cb) {
@@ -874,7 +876,18 @@ extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rule
   const int G = p->q_heads / p->kv_heads;
   score_scales(p->scale, rules ? rules->cap : 0.0f, A);
   const bool cap = A.cap > 0.0f, bias = A.slopes != nullptr;
-  launch_attention<8>(A, G, cap, bias, (hipStream_t)stream);
+  // Waves per block: eight share each K and V row, four (two blocks to a CU) leave a
+  // shorter tail and wait less for each other.  Eight only for long prompts, or groups that
+  // fill a block with few query tiles, while there are blocks enough.  Measured
+  // (us, eight -> four): 1 x 32/8 heads x 4096 143 -> 163, 2 x 32 x 8192 1141 -> 1190,
+  // packed documents 16 x 32/8 x 2011 343 -> 363, but 2 x 40 x 1531 91 -> 77,
+  // 8 x 32 x 2048 404 -> 387, 1 x 8 x 8192 198 -> 186; with a bias (more registers), 8 x 32 x
+  // 2048 525 -> 476, 2 x 32 x 8192 1467 -> 1452.
+  const int64_t blocks = (int64_t)p->batch * p->q_heads * ((p->tokens + 255) / 256);
+  if (!bias && (p->tokens >= 4096 ? blocks >= 512 : G >= 4 && blocks >= 1024))
+    launch_attention<8>(A, G, cap, bias, (hipStream_t)stream);
+  else
+    launch_attention<4>(A, G, cap, bias, (hipStream_t)stream);
   return check_launch(who);
 }
 
