@@ -565,17 +565,20 @@ void prompt_attention_kernel(PromptArgs A) {
 }
 
 // H2O importance under the rules: a wave holds 64 keys of one KV head and streams
-// the queries of every head of the group past them (queries along the tile's
-// columns, so a lane holds one query per tile, whose log-sum-exp and interval are
-// scalars), as prefill_colsum_kernel does for the causal case.  WS waves of the
-// block take the same keys and share out the 32-query subtiles.
+// the queries of one query head past them (queries along the tile's columns, so a
+// lane holds one query per tile, whose log-sum-exp and interval are scalars), as
+// prefill_colsum_kernel does for the causal case.  WS waves of the block take the
+// same keys and share out the 32-query subtiles.  The heads of a group have blocks
+// of their own and are added up afterwards in head order: with documents the
+// longest block, not the work, is the launch (8 x 32/8 x 4096, documents of up to 2500 tokens:
+// 541 us; all four heads in one block 717).
 struct SumArgs {
   const uint16_t *q, *k;
   int64_t qs[3], ks[3];
   const float *lse, *slopes;
   const int32_t *begin, *end;
   const int4 *spans;  // of every 32 queries, or NULL (causal)
-  float *scores;
+  float *sums;  // [batch, q_heads, T]
   int window;
   int q_heads, kv_heads, units, nblk, run, T;
   float scale, cap;
@@ -623,10 +626,11 @@ void prompt_colsum_kernel(SumArgs A) {
   const int wc = wave / WS, ws = wave % WS;
   const int G = A.q_heads / A.kv_heads, T = A.T, nsub = (T + 31) / 32;
   int hk, idx;
-  if (!block_unit(A.units, A.nblk, A.run, hk, idx)) return;
-  const int b = hk / A.kv_heads, kvh = hk % A.kv_heads;
-  const int j_base = idx * kKeys, j_wave = j_base + kWaveRows * wc;
-  const uint16_t *qb = A.q + b * A.qs[0] + (int64_t)kvh * G * A.qs[1], *kb = A.k + b * A.ks[0] + kvh * A.ks[1];
+  if (!block_unit(A.units, A.nblk * G, A.run, hk, idx)) return;
+  const int b = hk / A.kv_heads, kvh = hk % A.kv_heads, head = kvh * G + idx % G;
+  const int j_base = idx / G * kKeys, j_wave = j_base + kWaveRows * wc;
+  const int64_t row = ((int64_t)b * A.q_heads + head) * T;  // of lse and sums
+  const uint16_t *qb = A.q + b * A.qs[0] + head * A.qs[1], *kb = A.k + b * A.ks[0] + kvh * A.ks[1];
   auto sub_span = [&](int sub) {
     if (sub >= nsub) return make_int4(T, 0, 0, 0);
     return A.spans ? A.spans[(int64_t)b * nsub + sub] : causal_span(32 * sub, T);
@@ -668,14 +672,13 @@ void prompt_colsum_kernel(SumArgs A) {
   float r_lse = 0.0f;
   int2 r_span = make_int2(0, 0);
   int4 r_sub = make_int4(0, 0, 0, 0);
-  auto load = [&](int buf, int g, int t) {
-    const uint16_t *rows = qb + g * A.qs[1];
+  auto load = [&](int buf, int t) {
 #pragma unroll
     for (int u = 0; u < TR / 64; ++u)
-      stage_rows<4>(s_rows[buf] + 64 * u * kRowWords, rows, A.qs[2], t * TR + 64 * u, T, q_off);
+      stage_rows<4>(s_rows[buf] + 64 * u * kRowWords, qb, A.qs[2], t * TR + 64 * u, T, q_off);
     if (tid < TR) {
       const int i = t * TR + tid, ic = min(i, T - 1);
-      r_lse = A.lse[((int64_t)b * A.q_heads + kvh * G + g) * T + ic] * kLog2e;
+      r_lse = A.lse[row + ic] * kLog2e;
       int lo, hi;
       query_span(A.begin, A.end, A.window, (int64_t)b * T + ic, ic, T, lo, hi);
       r_span = i < T ? make_int2(lo, hi) : make_int2(0, 0);
@@ -693,64 +696,61 @@ void prompt_colsum_kernel(SumArgs A) {
   };
   const uint32_t off = tile_offset();
   if (t_first < t_end) {
-    load(0, 0, t_first);
+    load(0, t_first);
     commit(0);
     int buf = 0;
-    for (int g = 0; g < G; ++g) {
-      const float slope = BIAS ? A.slopes[kvh * G + g] * kLog2e : 0.0f;
-      for (int t = t_first; t < t_end; ++t) {
-        const u4_t *rows = s_rows[buf];
+    const float slope = BIAS ? A.slopes[head] * kLog2e : 0.0f;
+    for (int t = t_first; t < t_end; ++t) {
+      const u4_t *rows = s_rows[buf];
 #pragma unroll
-        for (int s = 0; s < SUBS; ++s) {
-          const int sub = ws * SUBS + s, i0 = t * TR + 32 * sub;
-          const int4 sp = s_sub[buf][sub];
-          const int any_lo = __builtin_amdgcn_readfirstlane(sp.x), any_hi = __builtin_amdgcn_readfirstlane(sp.y);
-          const int full_lo = __builtin_amdgcn_readfirstlane(sp.z), full_hi = __builtin_amdgcn_readfirstlane(sp.w);
-          u4_t bq[8];
-          read_tile(rows, off, 32 * sub, bq);
-          const float lse2 = s_lse[buf][32 * sub + n];
-          const int2 span = s_span[buf][32 * sub + n];
-          if (s == SUBS - 1) {  // after the tile's last LDS read: the compiler holds LDS reads back for loads to LDS
-            const bool wrap = t + 1 == t_end;
-            load(buf ^ 1, wrap ? min(g + 1, G - 1) : g, wrap ? t_first : t + 1);
+      for (int s = 0; s < SUBS; ++s) {
+        const int sub = ws * SUBS + s, i0 = t * TR + 32 * sub;
+        const int4 sp = s_sub[buf][sub];
+        const int any_lo = __builtin_amdgcn_readfirstlane(sp.x), any_hi = __builtin_amdgcn_readfirstlane(sp.y);
+        const int full_lo = __builtin_amdgcn_readfirstlane(sp.z), full_hi = __builtin_amdgcn_readfirstlane(sp.w);
+        u4_t bq[8];
+        read_tile(rows, off, 32 * sub, bq);
+        const float lse2 = s_lse[buf][32 * sub + n];
+        const int2 span = s_span[buf][32 * sub + n];
+        if (s == SUBS - 1) {  // after the tile's last LDS read: the compiler holds LDS reads back for loads to LDS
+          load(buf ^ 1, min(t + 1, t_end - 1));
+        }
+        if (any_lo >= j_wave + kWaveRows || any_hi <= j_wave) continue;  // wave-uniform
+        const int i = min(i0 + n, T - 1);
+#pragma unroll
+        for (int cb = 0; cb < 2; ++cb) {
+          const int j0 = j_wave + 32 * cb;
+          const f16_t d = logits(ak[cb], bq);
+          bool full = j0 >= full_lo && j0 + 32 <= full_hi;
+          if constexpr (BIAS) full = full && (j0 + 31 <= i0 || j0 > i0 + 31);
+          if constexpr (CAP) {
+            float big = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(d[r]));
+            full = full && !__ballot(!(big < A.poly.limit));
           }
-          if (any_lo >= j_wave + kWaveRows || any_hi <= j_wave) continue;  // wave-uniform
-          const int i = min(i0 + n, T - 1);
-#pragma unroll
-          for (int cb = 0; cb < 2; ++cb) {
-            const int j0 = j_wave + 32 * cb;
-            const f16_t d = logits(ak[cb], bq);
-            bool full = j0 >= full_lo && j0 + 32 <= full_hi;
-            if constexpr (BIAS) full = full && (j0 + 31 <= i0 || j0 > i0 + 31);
-            if constexpr (CAP) {
-              float big = 0.0f;
-#pragma unroll
-              for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(d[r]));
-              full = full && !__ballot(!(big < A.poly.limit));
+          if (full) {
+            Coef c = {0.0f, -lse2, A.scale, 0.0f, A.poly};
+            if constexpr (BIAS) {
+              c.slope = j0 > i0 ? -slope : slope;
+              c.base = fmaf(c.slope, (float)(j0 + 4 * half - i), c.base);
             }
-            if (full) {
-              Coef c = {0.0f, -lse2, A.scale, 0.0f, A.poly};
-              if constexpr (BIAS) {
-                c.slope = j0 > i0 ? -slope : slope;
-                c.base = fmaf(c.slope, (float)(j0 + 4 * half - i), c.base);
-              }
 #pragma unroll
-              for (int r = 0; r < 16; ++r) cs[cb][r] += __builtin_amdgcn_exp2f(term<CAP, BIAS>(d[r], r, c));
-            } else {
+            for (int r = 0; r < 16; ++r) cs[cb][r] += __builtin_amdgcn_exp2f(term<CAP, BIAS>(d[r], r, c));
+          } else {
 #pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const int j = j0 + tile_row(r);
-                float x = CAP ? tanh_fine(d[r] * A.scale) * A.cap : d[r] * A.scale;
-                if constexpr (BIAS) x = fmaf(-slope, (float)abs(i - j), x);
-                const float p = __builtin_amdgcn_exp2f(x - lse2);
-                cs[cb][r] += j >= span.x && j < span.y ? p : 0.0f;
-              }
+            for (int r = 0; r < 16; ++r) {
+              const int j = j0 + tile_row(r);
+              float x = CAP ? tanh_fine(d[r] * A.scale) * A.cap : d[r] * A.scale;
+              if constexpr (BIAS) x = fmaf(-slope, (float)abs(i - j), x);
+              const float p = __builtin_amdgcn_exp2f(x - lse2);
+              cs[cb][r] += j >= span.x && j < span.y ? p : 0.0f;
             }
           }
         }
-        buf ^= 1;
-        commit(buf);
       }
+      buf ^= 1;
+      commit(buf);
     }
   }
   // over the tile's 32 query columns, then over the WS waves
@@ -769,7 +769,17 @@ void prompt_colsum_kernel(SumArgs A) {
 #pragma unroll
   for (int o = 1; o < WS; ++o) v += s_sum[wave + o][lane];
   const int kj = j_wave + lane;
-  if (kj < T) A.scores[(int64_t)hk * T + kj] = v;
+  if (kj < T) A.sums[row + kj] = v;
+}
+
+__global__ __launch_bounds__(256) void sum_heads_kernel(const float *sums, int G, int T, float *scores) {
+  const int j = blockIdx.x * 256 + threadIdx.x;
+  const int64_t hk = (int64_t)blockIdx.z * 65535 + blockIdx.y;
+  if (j >= T) return;
+  const float *p = sums + hk * G * T + j;
+  float v = p[0];
+  for (int g = 1; g < G; ++g) v += p[(int64_t)g * T];
+  scores[hk * T + j] = v;
 }
 
 // ---------------------------------------------------------------------------
@@ -891,9 +901,13 @@ extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rule
   return check_launch(who);
 }
 
+// Workspace: the intervals of every 32 queries, then, where heads share a KV head,
+// every query head's sums.
+static size_t spans_bytes(int32_t batch, int32_t tokens) { return (size_t)batch * (((size_t)tokens + 31) / 32) * sizeof(int4); }
+
 extern "C" size_t mikv_prompt_importance_workspace_size(int32_t batch, int32_t q_heads, int32_t kv_heads, int32_t tokens) {
   if (batch < 1 || q_heads < 1 || kv_heads < 1 || tokens < 1) return 0;
-  return (size_t)batch * (((size_t)tokens + 31) / 32) * sizeof(int4);
+  return spans_bytes(batch, tokens) + (q_heads > kv_heads ? (size_t)batch * q_heads * tokens * sizeof(float) : 0);
 }
 
 extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rules *rules, const float *lse, float *scores,
@@ -906,14 +920,17 @@ extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rul
     return set_error(MIKV_ERR_CAPACITY, "%s: workspace too small", who);
   if ((uintptr_t)ws % 16) return set_error(MIKV_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
   hipStream_t st = (hipStream_t)stream;
+  const int G = p->q_heads / p->kv_heads;
   SumArgs A{};
-  A.q = p->q, A.k = p->k, A.lse = lse, A.scores = scores;
+  A.q = p->q, A.k = p->k, A.lse = lse;
+  A.sums = G > 1 ? (float *)((char *)ws + spans_bytes(p->batch, p->tokens)) : scores;
   copy3(A.qs, p->q_stride), copy3(A.ks, p->k_stride);
   if (rules) A.slopes = rules->slopes, A.begin = rules->begin, A.end = rules->end, A.window = rules->window;
   A.q_heads = p->q_heads, A.kv_heads = p->kv_heads, A.T = p->tokens;
   A.units = p->batch * p->kv_heads;
   score_scales(p->scale, rules ? rules->cap : 0.0f, A);
-  if (A.begin || A.end || A.window) {
+  const bool spans = A.begin || A.end || A.window;
+  if (spans) {
     const int nsub = (p->tokens + 31) / 32;
     A.spans = (const int4 *)ws;
     for (int b = 0; b < p->batch; b += 65535)
@@ -921,18 +938,26 @@ extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rul
                          A.begin ? A.begin + (int64_t)b * p->tokens : nullptr, A.end ? A.end + (int64_t)b * p->tokens : nullptr,
                          A.window, p->tokens, nsub, (int4 *)ws + (int64_t)b * nsub);
   }
-  // waves on the same keys, by the blocks of 256 keys: as for the causal scores
-  // (plan_pass), fewer keys per block only while the grid leaves CUs idle
-  const int64_t n1 = (int64_t)A.units * ((p->tokens + 255) / 256);
-  const int ws_ = n1 >= 768 ? 1 : n1 >= 192 ? 2 : 4, keys = kWaveRows * 4 / ws_;
+  // Waves on the same keys, by the blocks of 256 keys (two fit a CU, 512 the chip): as for
+  // the causal scores (plan_pass), fewer keys per block only while the grid leaves CUs
+  // idle.  Measured with 1 / 2 / 4 waves on the same keys, us: 8 x 32/8 x 4096 (4096
+  // blocks) 705 / 864 / 1147, under documents and a cap 406 / 484 / 664; 1 x 40 x 1531
+  // (240) 53 / 38 / 44; 1 x 32 x 512 (64) 25 / 19 / 15.
+  const int64_t n1 = (int64_t)A.units * G * ((p->tokens + 255) / 256);
+  const int share = n1 >= 768 ? 1 : n1 >= 192 ? 2 : 4;
+  const int keys = kWaveRows * 4 / share;
   A.nblk = (p->tokens + keys - 1) / keys;
-  A.run = std::min(n1 >= 4096 ? 32 : 4, A.nblk);
-  const dim3 grid(grid_blocks(A.units, A.nblk, A.run));
-  if (ws_ == 1)
+  const int per_unit = A.nblk * G;
+  A.run = std::min(n1 >= 4096 ? 32 : 4, per_unit);
+  const dim3 grid(grid_blocks(A.units, per_unit, A.run));
+  if (share == 1)
     launch_colsum<1>(A, grid, st);
-  else if (ws_ == 2)
+  else if (share == 2)
     launch_colsum<2>(A, grid, st);
   else
     launch_colsum<4>(A, grid, st);
+  if (G > 1)
+    hipLaunchKernelGGL(sum_heads_kernel, dim3((p->tokens + 255) / 256, std::min(65535, A.units), (A.units + 65534) / 65535),
+                       dim3(256), 0, st, (const float *)A.sums, G, p->tokens, scores);
   return check_launch(who);
 }
