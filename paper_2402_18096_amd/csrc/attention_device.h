@@ -276,6 +276,65 @@ __device__ inline float token_sum(float v) {
   return v;
 }
 
+template <int CTRL>
+__device__ inline float dpp_mov(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+
+// Lanes whose number has bit `bit`, as a scalar mask (a compare would take a vector
+// instruction at every use).
+template <int BIT>
+__device__ inline bool lanes_with() {
+  return __builtin_amdgcn_inverse_ballot_w64(BIT == 1   ? 0xaaaaaaaaaaaaaaaaull
+                                             : BIT == 2 ? 0xccccccccccccccccull
+                                                        : 0xf0f0f0f0f0f0f0f0ull);
+}
+
+// token_sum of G values at once that leaves each lane only the sum of value
+// part % G: while a bit of `part` numbers values, a lane keeps the half that its bit names
+// and gives the other half away.  v[0] is the sum.
+template <int LPT, int G, int SPAN = LPT / 2, int N = G>
+__device__ inline float token_sum_own(float (&v)[G]) {
+  auto other = [](float x) { return dpp_mov<SPAN == 8 ? 0x140 : SPAN == 4 ? 0x141 : SPAN == 2 ? 0x4E : 0xB1>(x); };
+  if constexpr (SPAN == 0) {
+    return v[0];
+  } else if constexpr (SPAN < G) {
+    const bool up = lanes_with<SPAN>();
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) v[k] = (up ? v[k + N / 2] : v[k]) + other(up ? v[k] : v[k + N / 2]);
+    return token_sum_own<LPT, G, SPAN / 2, N / 2>(v);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] += other(v[k]);
+    return token_sum_own<LPT, G, SPAN / 2, N>(v);
+  }
+}
+
+// The other way: every lane gets the G values that the lanes part % G of its token hold.
+template <int G>
+__device__ inline void token_share(float own, float (&v)[G]) {
+  if constexpr (G == 1) {
+    v[0] = own;
+  } else if constexpr (G == 2) {
+    v[0] = dpp_mov<0xA0>(own);
+    v[1] = dpp_mov<0xF5>(own);
+  } else {
+    v[0] = dpp_mov<0x00>(own);
+    v[1] = dpp_mov<0x55>(own);
+    v[2] = dpp_mov<0xAA>(own);
+    v[3] = dpp_mov<0xFF>(own);
+    if constexpr (G == 8) {
+      const bool up = lanes_with<4>();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = dpp_mov<0x141>(v[i]);  // the other quad of the half-row
+        v[i + 4] = up ? v[i] : x;
+        v[i] = up ? x : v[i];
+      }
+    }
+  }
+}
+
 // Sum over the 64/LPT lanes that hold the same `part` (same channels,
 // different tokens): rotations inside each 16-lane row, shuffles across rows.
 template <int LPT>
@@ -371,13 +430,19 @@ __device__ inline void load_seg_rows(Rows<BITS, CPL> &r, rsrc_t rk, rsrc_t rv, r
 // keeps q_c * alpha_c (times the code class factor) and sum_c q_c beta_c for
 // the block of its current token and refreshes them when the block changes.
 // RULES: scores under A.rules.  A token's position comes with its key; one that is
-// hidden gets a score of -inf and adds nothing, whatever its row holds.
+// hidden gets a score of -inf and adds nothing, whatever its row holds.  The lanes of
+// a token share out its G scores (lane part % G keeps one): a rule and an
+// exponential per lane, not G of them (16 x 32/8 x 8192, fp16 over INT4, under a cap:
+// every lane scoring every head 104 us, this 78, and 78 without rules).  Chunks run
+// backwards, so that under a bias by distance the first scores are the largest and the
+// running maximum stays (16 x 32/8 x 16384, fp16 over INT2: forwards 98 us, both 84).
 template <int BITS, int G, int CPL, bool SPLITQ, int UNROLL, int PREFETCH, bool KPC = false, bool STREAM = false, bool RULES = false>
 __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, bool is_hi, float *s_lds) {
   using F = Fmt<BITS>;
   using FK = Fmt<BITS, RULES && !KPC>;  // keys (the per-channel ones enter fp32 FMAs, which are exact)
   constexpr int LPT = kHeadDim / CPL, TPW = 64 / LPT, NP = CPL / 2;
   constexpr bool Q = F::kQuant;
+  constexpr int S = RULES ? 1 : G;  // scores, maxima and sums a lane keeps
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int part = lane % LPT, tsub = lane / LPT;
   const int b = h / A.kv_heads, kvh = h % A.kv_heads;
@@ -405,11 +470,15 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
   // each pair scaled by 2^(qshift - cls) (query_shift); with SPLITQ a second
   // fp16 pair carries the rounding remainder.  qsum24 = 2^(qshift - 24) * the
   // sum of the lane's query channels (fp32).
-  float m2[G], l[G], bsum[G], o[G][CPL];
+  float m2[S], l[S], bsum[G], o[G][CPL];
+  const int own = RULES ? part % G : 0;  // this lane's query head
 #pragma unroll
-  for (int i = 0; i < G; ++i) {
+  for (int i = 0; i < S; ++i) {
     m2[i] = kNegInf;
     l[i] = 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
     bsum[i] = 0.0f;
 #pragma unroll
     for (int c = 0; c < CPL; ++c) o[i][c] = 0.0f;
@@ -468,6 +537,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
   // zero without a memory access, so a load needs no branch around it.
   const rsrc_t r_none = make_rsrc(kb, 0u);
   auto load_part = [&](auto which, Rows<BITS, CPL>(&r)[UNROLL], int it, bool live = true) {
+    if constexpr (RULES) it = n_iter - 1 - it;
     const uint32_t orow = off_row0 + (uint32_t)(it * kPerIter) * (uint32_t)kRow;
     const uint32_t opar = off_par0 + (uint32_t)(it * kPerIter) * (uint32_t)ng * 4u;
     const uint32_t okp = KPC ? off_kp0 + (uint32_t)(it * kPerIter) * 4u : opar;
@@ -546,13 +616,12 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
     qshift = query_shift<kMaxCls, kMinCls>(bound);
   }
   const float s2scale_q = Q ? __builtin_ldexpf(s2scale, 24 - qshift) : s2scale;
-  float arg_scale = 0.0f, slope2[RULES ? G : 1];
+  float arg_scale = 0.0f, slope2 = 0.0f;
   int begin = 0;
   if constexpr (RULES) {
     arg_scale = Q ? __builtin_ldexpf(A.rules.cap_scale, 24 - qshift) : A.rules.cap_scale;
     begin = rule_begin(A.rules, b);
-#pragma unroll
-    for (int i = 0; i < G; ++i) slope2[i] = A.rules.slopes ? A.rules.slopes[kvh * G + i] * kLog2e : 0.0f;
+    if (A.rules.slopes) slope2 = A.rules.slopes[kvh * G + own] * kLog2e;
   }
 #pragma unroll
   for (int i = 0; i < G; ++i) {
@@ -632,11 +701,12 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
     }
   };
 
-  float s2[UNROLL][G];
+  float s2[UNROLL][S];
+  bool valid[UNROLL];
   // Scores of one iteration (and the lazy running-max update).
   auto proc_k = [&](Rows<BITS, CPL>(&cur)[UNROLL], int it) {
-    bool valid[UNROLL];
     uint64_t raise = 0;  // lanes whose score passes the lazy threshold (a ballot per token)
+    if constexpr (RULES) it = n_iter - 1 - it;
     const int rem = end - it * kPerIter;  // wave-uniform: a token is valid when first + u * TPW < rem
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
@@ -652,6 +722,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
         const int blk = min(max((int)cur[u].kp / kKeyBlock, 0), max(A.n_kblk - 1, 0));
         if (blk != kblk) kpc_refresh(blk);
       }
+      float sums[G];
 #pragma unroll
       for (int i = 0; i < G; ++i) {
         float d = 0.0f;
@@ -677,23 +748,49 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
         // the final scale, so the result is the same bits
         float s = KPC ? d + b24[i] : Q ? fmaf((float)kab.x, d, fmaf((float)kab.y, qsum24[i], 0.0f)) : d;
         if constexpr (RULES) {
-          const float dot = token_sum<LPT>(s);
-          s = rule_score(A.rules, dot * s2scale_q, dot * arg_scale, slope2[i], (int)cur[u].pos);
-        } else {
-          s = token_sum<LPT>(s) * s2scale_q;
+          sums[i] = s;
+          continue;
         }
+        s = token_sum<LPT>(s) * s2scale_q;
         s = valid[u] ? s : kNegInf;
-        s2[u][i] = s;
+        s2[u][i % S] = s;
         // every lane of the token holds s: all of them store it (same
         // value, same address), which keeps the loop free of exec-mask
         // branches around the store
         s_lds[i * max_chunk(G) + it * kPerIter + u * TPW + tsub] = s;
-        raise |= __ballot(s > m2[i] + kLazy);
+        raise |= __ballot(s > m2[i % S] + kLazy);
+      }
+      if constexpr (RULES) {
+        const float dot = token_sum_own<LPT, G>(sums);
+        float s = rule_score(A.rules, dot * s2scale_q, dot * arg_scale, slope2, (int)cur[u].pos);
+        s = valid[u] ? s : kNegInf;
+        s2[u][0] = s;
+        s_lds[own * max_chunk(G) + it * kPerIter + u * TPW + tsub] = s;
+        raise |= __ballot(s > m2[0] + kLazy);
       }
     }
-    if (raise) {
+    if constexpr (RULES) {
+      if (raise) {
+        float mx = s2[0][0], f[G];
 #pragma unroll
-      for (int i = 0; i < G; ++i) {
+        for (int u = 1; u < UNROLL; ++u) mx = fmaxf(mx, s2[u][0]);
+#pragma unroll
+        for (int o = G; o < 64; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o, 64));  // over the lanes of this head
+        mx = fmaxf(mx, m2[0]);
+        const float fo = m2[0] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m2[0] - mx);
+        m2[0] = mx;
+        l[0] *= fo;
+        token_share<G>(fo, f);
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+          bsum[i] *= f[i];
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) o[i][c] *= f[i];
+        }
+      }
+    } else if (raise) {
+#pragma unroll
+      for (int i = 0; i < S; ++i) {
         float mx = s2[0][i];
 #pragma unroll
         for (int u = 1; u < UNROLL; ++u) mx = fmaxf(mx, s2[u][i]);
@@ -713,12 +810,10 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
   auto proc_v = [&](Rows<BITS, CPL>(&cur)[UNROLL]) {
     // RULES: until a visible token raises it the maximum stays at -inf, where
     // every score is, too
-    float ref[G];
-#pragma unroll
-    for (int i = 0; i < G; ++i) ref[i] = RULES && m2[i] == kNegInf ? 0.0f : m2[i];
+    const float ref = RULES && m2[0] == kNegInf ? 0.0f : m2[0];
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
-      const bool hidden = RULES && s2[u][0] == kNegInf;
+      const bool hidden = RULES && !valid[u];
       uint32_t vx[NP], vraw[Rows<BITS, CPL>::KW];
       seg_words(cur[u].v, vraw);
       F::template unpack<CPL>(vraw, vx);
@@ -727,12 +822,18 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
         for (int p = 0; p < NP; ++p) vx[p] = hidden ? 0u : vx[p];
       }
       const half2_t vab = as_h2(hidden ? 0u : cur[u].vp);  // (alpha, beta) of the value group
+      float shared[G];
+      if constexpr (RULES) {
+        const float e = __builtin_amdgcn_exp2f(s2[u][0] - ref);
+        l[0] += e;
+        token_share<G>(e, shared);
+      }
 #pragma unroll
       for (int i = 0; i < G; ++i) {
         // past the pool s2 = -inf, and m2 is finite from the first iteration
         // on (its first token is valid and raises the max), so e = 0
-        const float e = __builtin_amdgcn_exp2f(s2[u][i] - ref[i]);
-        l[i] += e;
+        const float e = RULES ? shared[i] : __builtin_amdgcn_exp2f(s2[u][i % S] - m2[i % S]);
+        if constexpr (!RULES) l[i % S] += e;
         const float w = Q ? fmaf(e, (float)vab.x, 0.0f) : e;
         if constexpr (Q) bsum[i] = fmaf(e, (float)vab.y, bsum[i]);
 #pragma unroll
@@ -813,17 +914,22 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
         o[i][F::hi(p)] = fmaf(o[i][F::hi(p)], sc, bsum[i]);
       }
     }
-    l[i] = wave_sum(l[i]) * (1.0f / LPT);  // every lane of a token added its e
+    if constexpr (!RULES) l[i % S] = wave_sum(l[i % S]) * (1.0f / LPT);  // every lane of a token added its e
 #pragma unroll
     for (int c = 0; c < CPL; ++c) o[i][c] = sum_token_lanes<LPT>(o[i][c]);
+  }
+  if constexpr (RULES) {  // over the lanes of this lane's head, LPT / G of them per token
+#pragma unroll
+    for (int x = G; x < 64; x *= 2) l[0] += __shfl_xor(l[0], x, 64);
+    l[0] *= (float)G / LPT;
   }
   const int nc = A.nc_hi + A.nc_lo;
 #pragma unroll
   for (int i = 0; i < G; ++i) {
     float *rec = A.partials + ((int64_t)(qh0 + i) * nc + rec_chunk) * kRec;
-    if (lane == 0) {
-      rec[0] = m2[i];
-      rec[1] = l[i];
+    if (lane == (RULES ? i : 0)) {
+      rec[0] = m2[i % S];
+      rec[1] = l[i % S];
       rec[kRecN] = __builtin_bit_cast(float, n_pool);
     }
     if (tsub == 0) {
@@ -945,7 +1051,7 @@ __device__ void attn_chunk_int2(const AttnArgs &A, int h, int chunk, int rec_chu
   // descriptor (zero, no memory access), so no branch is needed around it.
   const rsrc_t r_none = make_rsrc(A.lo_k, 0u);
   auto load = [&](Ld &d, int it, bool keys, bool vals, bool live) {
-    const uint32_t t0 = (uint32_t)(start + it * kItTok);
+    const uint32_t t0 = (uint32_t)(start + (RULES ? n_iter - 1 - it : it) * kItTok);
     const rsrc_t ak = live ? rk : r_none, av = live ? rv : r_none;
     const rsrc_t akp = live ? rkp : r_none, avp = live ? rvp : r_none;
 #pragma unroll
@@ -1138,7 +1244,7 @@ __device__ void attn_chunk_int2(const AttnArgs &A, int h, int chunk, int rec_chu
   // loaded once the scores are done, its values once the value MFMAs are.
   for (int it = 0; it < n_iter; ++it) {
     const bool live = it + 1 < n_iter;
-    const int t0 = start + it * kItTok;
+    const int t0 = start + (RULES ? n_iter - 1 - it : it) * kItTok;
     // --- scores of the four key tiles
     float s2[kKT][NSET];
     uint64_t raise = 0;
