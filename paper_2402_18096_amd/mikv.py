@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 import os
 from ctypes import c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 from typing import Optional
@@ -114,17 +115,17 @@ class PromptDesc(ctypes.Structure):
                 ("q_stride", c_int64 * 3), ("k_stride", c_int64 * 3), ("v_stride", c_int64 * 3)]
 
 
-_PR, _PP = ctypes.POINTER(RulesDesc), ctypes.POINTER(PromptDesc)
+_PR = ctypes.POINTER(RulesDesc)
 
 _LAYER_SIGS = {
     "mikv_rotary_frequencies": (c_int32, [ctypes.POINTER(RotaryScheme), ctypes.POINTER(ctypes.c_uint64),
                                           ctypes.POINTER(c_float)]),
-    "mikv_rotary": (c_int32, [ctypes.POINTER(Heads), c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p,
+    "mikv_rotary": (c_int32, [c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_void_p,
                               c_int32, c_void_p, c_int32, c_int32, c_float, c_void_p]),
     "mikv_mask_spans": (c_int32, [c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
-    "mikv_prompt_attention": (c_int32, [_PP, _PR, c_void_p, ctypes.POINTER(c_int64), c_void_p, c_void_p]),
+    "mikv_prompt_attention": (c_int32, [c_void_p, _PR, c_void_p, ctypes.POINTER(c_int64), c_void_p, c_void_p]),
     "mikv_prompt_importance_workspace_size": (c_size_t, [c_int32, c_int32, c_int32, c_int32]),
-    "mikv_prompt_importance": (c_int32, [_PP, _PR, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "mikv_prompt_importance": (c_int32, [c_void_p, _PR, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
 }
 
 for _n, _at in (("mikv_decode_attention", 5), ("mikv_decode_step", 7)):  # the rules follow the scale
@@ -484,18 +485,32 @@ _TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "bands": 3, "yarn": 4}
 
 
+# struct mikv_heads and struct mikv_prompt, packed in one call (filling the ctypes mirrors field by
+# field costs several times as much: a rotary call of three tensors 16 -> 12 us of host time)
+_HEADS, _PROMPT = struct.Struct("2P6q2i"), struct.Struct("5if3P9q")
+
+
 def _rows(t: torch.Tensor, shape, name: str):
     """Strides (batch, head, token) of [B, H, T, 128] rows, whose channels have to be contiguous.  A
     dimension of one element has no stride of its own."""
-    if t.dim() != 4 or t.shape[3] != HEAD_DIM or (shape is not None and t.shape != shape):
+    s = t.shape
+    if len(s) != 4 or s[3] != HEAD_DIM or (shape is not None and s != shape):
         raise MikvError(f"{name}: expected shape {tuple(shape) if shape else ('B', 'H', 'T', HEAD_DIM)}, "
-                        f"got {tuple(t.shape)}")
+                        f"got {tuple(s)}")
     if not t.is_cuda:
         raise MikvError(f"{name}: must be a device tensor")
-    st = t.stride()
-    if st[3] != 1:
+    x, y, z, c = t.stride()
+    if c != 1:
         raise MikvError(f"{name}: channels must be contiguous")
-    return [st[i] if t.shape[i] > 1 else 0 for i in range(3)]
+    return (x if s[0] > 1 else 0, y if s[1] > 1 else 0, z if s[2] > 1 else 0)
+
+
+def _here(name: str, *tensors):
+    """The tensors have to be on the current device, whose current stream takes the launch."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise MikvError(f"{name}: tensors must be on the current device")
 
 
 class MikvRotary:
@@ -528,21 +543,21 @@ def mikv_rotary(rotary: MikvRotary, xs, ys, positions: Optional[torch.Tensor] = 
     n = len(xs)
     if not 1 <= n <= 3 or len(ys) != n or len(rotate) < n:
         raise MikvError("mikv_rotary: one to three tensors, and as many outputs, expected")
-    B, _, T, _ = xs[0].shape if xs[0].dim() == 4 else (0, 0, 0, 0)
-    arr = (Heads * n)()
-    for i, (x, y) in enumerate(zip(xs, ys)):
-        if x.dim() != 4 or x.shape[0] != B or x.shape[2] != T:
+    x_type, y_type = _TYPES.get(xs[0].dtype), _TYPES.get(ys[0].dtype)
+    tensors = []
+    for x, y, turn in zip(xs, ys, rotate):
+        st, shape = _rows(x, None, "x"), x.shape
+        if shape[0] != xs[0].shape[0] or shape[2] != xs[0].shape[2]:
             raise MikvError("mikv_rotary: [B, H, T, 128] tensors of the same tokens expected")
-        if x.dtype is not xs[0].dtype or y.dtype is not ys[0].dtype or x.dtype not in _TYPES or y.dtype not in _TYPES:
+        if x.dtype is not xs[0].dtype or y.dtype is not ys[0].dtype or x_type is None or y_type is None:
             raise MikvError("mikv_rotary: one input and one output type of fp16, bf16 and fp32 expected")
-        h = arr[i]
-        h.x, h.y, h.heads, h.rotate = x.data_ptr(), y.data_ptr(), x.shape[1], int(bool(rotate[i]))
-        h.x_stride[:] = _rows(x, None, "x")
-        h.y_stride[:] = _rows(y, x.shape, "y")
+        tensors.append(_HEADS.pack(x.data_ptr(), y.data_ptr(), *st, *_rows(y, shape, "y"), shape[1], bool(turn)))
+    B, _, T, _ = xs[0].shape
     if positions is not None:
         _require(positions, torch.int32, (B, T), "positions")
-    _check(lib().mikv_rotary(arr, n, B, T, HEAD_DIM, _TYPES[xs[0].dtype], _TYPES[ys[0].dtype], _ptr(positions), pos0,
-                             _ptr(rotary.freq), rotary.rot_dim, int(rotary.interleaved), rotary.magnitude, _stream()),
+    _here("mikv_rotary", rotary.freq, positions, *xs, *ys)
+    _check(lib().mikv_rotary(b"".join(tensors), n, B, T, HEAD_DIM, x_type, y_type, _ptr(positions), pos0,
+                             _ptr(rotary.freq), rotary.rot_dim, rotary.interleaved, rotary.magnitude, _stream()),
            "mikv_rotary")
 
 
@@ -564,6 +579,10 @@ class ScoreRules:
         return RulesDesc(self.cap, _ptr(self.slopes), _ptr(self.begin), _ptr(self.end), self.window)
 
 
+def _held(rules: Optional[ScoreRules]):
+    return () if rules is None else (rules.slopes, rules.begin, rules.end)
+
+
 def mikv_mask_spans(begin: torch.Tensor, end: torch.Tensor, documents: Optional[torch.Tensor] = None,
                     prefix: Optional[torch.Tensor] = None, window: int = 0):
     """The keys [begin, end) that each query of a prompt sees, int32 [B, T]: those of its document (a run of equal
@@ -578,6 +597,7 @@ def mikv_mask_spans(begin: torch.Tensor, end: torch.Tensor, documents: Optional[
         _require(documents, torch.int32, (B, T), "documents")
     if prefix is not None:
         _require(prefix, torch.int32, (B,), "prefix")
+    _here("mikv_mask_spans", begin, end, documents, prefix)
     _check(lib().mikv_mask_spans(_ptr(documents), _ptr(prefix), B, T, window, _ptr(begin), _ptr(end), _stream()),
            "mikv_mask_spans")
 
@@ -585,15 +605,15 @@ def mikv_mask_spans(begin: torch.Tensor, end: torch.Tensor, documents: Optional[
 def _prompt(q, k, v, scale):
     if q.dim() != 4 or k.dim() != 4:
         raise MikvError("q [B, Hq, T, 128] and k [B, Hkv, T, 128] expected")
-    B, Hq, T, D = q.shape
-    p = PromptDesc(B, Hq, k.shape[1], T, D, 1.0 / math.sqrt(HEAD_DIM) if scale is None else scale)
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        if t is None:
-            continue
-        _require(t, torch.float16, name=name)
-        setattr(p, name, t.data_ptr())
-        getattr(p, name + "_stride")[:] = _rows(t, q.shape if name == "q" else (B, k.shape[1], T, D), name)
-    return p
+    (B, Hq, T, D), Hkv = q.shape, k.shape[1]
+    _require(q, torch.float16, name="q")
+    _require(k, torch.float16, name="k")
+    qs, ks, vs = _rows(q, q.shape, "q"), _rows(k, (B, Hkv, T, D), "k"), (0, 0, 0)
+    if v is not None:
+        _require(v, torch.float16, name="v")
+        vs = _rows(v, k.shape, "v")
+    return _PROMPT.pack(B, Hq, Hkv, T, D, 1.0 / math.sqrt(HEAD_DIM) if scale is None else scale, q.data_ptr(),
+                        k.data_ptr(), 0 if v is None else v.data_ptr(), *qs, *ks, *vs)
 
 
 def mikv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
@@ -607,7 +627,8 @@ def mikv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
     if lse is not None:
         _require(lse, torch.float32, q.shape[:3], "lse")
     r = None if rules is None else ctypes.byref(rules.desc(q.shape[1], (q.shape[0], q.shape[2])))
-    _check(lib().mikv_prompt_attention(ctypes.byref(p), r, out.data_ptr(), stride, _ptr(lse), _stream()),
+    _here("mikv_prompt_attention", q, k, v, out, lse, *_held(rules))
+    _check(lib().mikv_prompt_attention(p, r, out.data_ptr(), stride, _ptr(lse), _stream()),
            "mikv_prompt_attention")
 
 
@@ -628,7 +649,8 @@ def mikv_prompt_importance(q: torch.Tensor, k: torch.Tensor, lse: torch.Tensor, 
     if ws is None:
         ws = _workspace(mikv_prompt_importance_workspace_size(B, Hq, k.shape[1], T), q.device)
     r = None if rules is None else ctypes.byref(rules.desc(Hq, (B, T)))
-    _check(lib().mikv_prompt_importance(ctypes.byref(p), r, _ptr(lse), _ptr(scores), _ptr(ws), ws.numel(), _stream()),
+    _here("mikv_prompt_importance", q, k, lse, scores, ws, *_held(rules))
+    _check(lib().mikv_prompt_importance(p, r, _ptr(lse), _ptr(scores), _ptr(ws), ws.numel(), _stream()),
            "mikv_prompt_importance")
 
 
@@ -639,6 +661,7 @@ def _decode_rules(rules: Optional[ScoreRules], cache: MikvCache):
 def mikv_decode_attention_scored(cache, length, q, out, probs_hi=None, probs_lo=None, rules: Optional[ScoreRules] = None,
                                  balance=None, scale=None, flags=0, workspace=None):
     """mikv_decode_attention under score rules."""
+    _here("mikv_decode_attention_scored", q, out, cache.n_hi, *_held(rules))
     _attention("mikv_decode_attention_scored", cache, length, q, out, probs_hi, probs_lo, balance, scale, flags, workspace,
                _decode_rules(rules, cache))
 
@@ -647,6 +670,7 @@ def mikv_decode_step_scored(cache: MikvCache, length: int, q, k_new, v_new, out,
                             probs_hi=None, probs_lo=None, rules: Optional[ScoreRules] = None, balance=None, scale=None,
                             flags=0, workspace=None, phase_events=None):
     """mikv_decode_step under score rules."""
+    _here("mikv_decode_step_scored", q, k_new, v_new, out, cache.n_hi, *_held(rules))
     _decode_step("mikv_decode_step_scored", cache, length, q, k_new, v_new, out, k_heavy, window, probs_hi, probs_lo, balance,
                  scale, flags, workspace, phase_events, _decode_rules(rules, cache))
 

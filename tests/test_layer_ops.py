@@ -642,6 +642,27 @@ def test_binding_refusals():
         mikv.mikv_mask_spans(torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32))
 
 
+def test_packed_descriptors_have_the_mirrors_layout():
+    h = mikv.Heads.from_buffer_copy(mikv._HEADS.pack(16, 32, 1, 2, 3, 4, 5, 6, 7, 1))
+    assert (h.x, h.y, list(h.x_stride), list(h.y_stride), h.heads, h.rotate) == (16, 32, [1, 2, 3], [4, 5, 6], 7, 1)
+    p = mikv.PromptDesc.from_buffer_copy(mikv._PROMPT.pack(1, 2, 3, 4, 128, 0.5, 16, 32, 0, *range(9)))
+    assert (p.batch, p.q_heads, p.kv_heads, p.tokens, p.head_dim, p.scale, p.q, p.k, p.v) == (1, 2, 3, 4, 128, 0.5, 16, 32, None)
+    assert [*p.q_stride, *p.k_stride, *p.v_stride] == list(range(9))
+
+
+@pytest.mark.gpu
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    x = torch.zeros(1, 2, 3, D, dtype=torch.float16, device="cuda")
+    spans = torch.zeros(1, 3, dtype=torch.int32, device="cuda")
+    lse, scores = torch.zeros(1, 2, 3, device="cuda"), torch.zeros(1, 2, 3, device="cuda")
+    rotary = mikv.MikvRotary()
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 7)
+    for call in (lambda: mikv.mikv_rotary(rotary, [x], [x]), lambda: mikv.mikv_mask_spans(spans, spans),
+                 lambda: mikv.mikv_prompt_attention(x, x, x, x), lambda: mikv.mikv_prompt_importance(x, x, lse, scores, workspace=spans)):
+        with pytest.raises(mikv.MikvError, match="current device"):
+            call()
+
+
 def test_every_declared_layer_symbol_is_bound():
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "mikv_layer.h")).read()
     names = set(re.findall(r"^(?:int|size_t) (mikv_\w+)\(", text, re.M))
