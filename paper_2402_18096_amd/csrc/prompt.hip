@@ -51,7 +51,7 @@ struct PromptArgs {
   const float *slopes;
   const int32_t *begin, *end;
   int window;
-  int q_heads, kv_heads, units, nblk, run, T;
+  int q_heads, kv_heads, units, parts, nblk, run, T;
   float scale, cap;  // scale: of the logit in log2 units (cap: to the argument of tanh); cap in log2 units
   CapPoly poly;
 };
@@ -243,6 +243,14 @@ __device__ inline void query_span(const int32_t *begin, const int32_t *end, int 
   if (lo >= hi) lo = hi = 0;
 }
 
+// block_unit with a unit's blocks dealt out to `parts` XCDs (unit_parts).
+__device__ inline bool block_of_unit(int units, int per_unit, int parts, int run, int &unit, int &idx) {
+  if (!block_unit(units * parts, (per_unit + parts - 1) / parts, run, unit, idx)) return false;
+  idx = idx * parts + unit % parts;
+  unit /= parts;
+  return idx < per_unit;
+}
+
 // A block of NW waves: min(G, NW) query heads of one KV head's group times the
 // 32-query tiles that fill it, so that its waves need the same keys as nearly as
 // they can.
@@ -259,7 +267,7 @@ void prompt_attention_kernel(PromptArgs A) {
   const int G = A.q_heads / A.kv_heads, T = A.T;
   const int hw = min(G, NW), rw = NW / hw, groups = G / hw;  // heads and query tiles of a block, head groups
   int hk, idx;
-  if (!block_unit(A.units, A.nblk * groups, A.run, hk, idx)) return;
+  if (!block_of_unit(A.units, A.nblk * groups, A.parts, A.run, hk, idx)) return;
   const int b = hk / A.kv_heads, kvh = hk % A.kv_heads, head = kvh * G + (idx % groups) * hw + wave % hw;
   const int i_wave = kWaveQueries * ((A.nblk - 1 - idx / groups) * rw + wave / hw);
   const uint16_t *kb = A.k + b * A.ks[0] + kvh * A.ks[1], *vb = A.v + b * A.vs[0] + kvh * A.vs[1];
@@ -379,9 +387,12 @@ void prompt_attention_kernel(PromptArgs A) {
     // LDS during the first subtile of tile t, its value rows during the second, each
     // fetched one subtile before.  (Past the last tile rows are loaded, or zeros,
     // and never used.)
+    // Under a bias the tiles go backwards: the first scores are then the largest (of
+    // the keys no later than the query), and the maximum is not raised at every tile.
+    auto tile = [&](int t) INLINE { return BIAS ? max(t_first + n_tiles - 1 - t, 0) : t_first + t; };
     u4_t rows[tile_loads<NW>()];
-    auto fetch_keys = [&](int t) INLINE { fetch_rows<NW>(rows, kb, A.ks[2], (t_first + t) * TR, T); };
-    auto fetch_values = [&](int t) INLINE { fetch_rows<NW>(rows, vb, A.vs[2], (t_first + t) * TR, T); };
+    auto fetch_keys = [&](int t) INLINE { fetch_rows<NW>(rows, kb, A.ks[2], tile(t) * TR, T); };
+    auto fetch_values = [&](int t) INLINE { fetch_rows<NW>(rows, vb, A.vs[2], tile(t) * TR, T); };
     auto feed_keys = [&](int t) INLINE {
       keep_rows<NW>(k_tile(t), rows, swz_k);
       fetch_values(t);
@@ -390,9 +401,14 @@ void prompt_attention_kernel(PromptArgs A) {
       keep_rows<NW>(v_tile(t), rows, swz_v);
       fetch_keys(t + 1);
     };
-    fetch_keys(0);
-    feed_keys(0);
-    feed_values(0);
+    {
+      u4_t values[tile_loads<NW>()];
+      fetch_keys(0);
+      fetch_rows<NW>(values, vb, A.vs[2], tile(0) * TR, T);
+      keep_rows<NW>(k_tile(0), rows, swz_k);
+      fetch_keys(1);
+      keep_rows<NW>(v_tile(0), values, swz_v);
+    }
     __syncthreads();
     // A tile that this wave does not see.  At the barrier the next tile's keys and
     // this one's value rows are complete, and every wave is done with the keys of the tile
@@ -405,8 +421,13 @@ void prompt_attention_kernel(PromptArgs A) {
 
     // The tiles that any query of this wave sees; for the others it only keeps step
     // with the block.
-    const int own_first = own_hi > own_lo ? own_lo / TR - t_first : 0;
-    const int own_end = own_hi > own_lo ? (own_hi + TR - 1) / TR - t_first : 0;
+    int own_first = own_hi > own_lo ? own_lo / TR - t_first : 0;
+    int own_end = own_hi > own_lo ? (own_hi + TR - 1) / TR - t_first : 0;
+    if constexpr (BIAS) {
+      const int first = own_first;
+      own_first = n_tiles - own_end;
+      own_end = n_tiles - first;
+    }
     for (int t = 0; t < own_first; ++t) idle(t);
 
     const uint32_t off = tile_offset(), voff = v_offset();
@@ -462,13 +483,13 @@ void prompt_attention_kernel(PromptArgs A) {
     // (those of the first tile come after the barrier), with weights of zero; infinities
     // and NaN are taken out of them unless every query sees them anyway.
     const int t_zero = max(own_first - 1, 0);
-    int j_was = (t_first + t_zero) * TR;
+    int j_was = tile(t_zero) * TR;
     const u4_t *v_was = v_tile(t_zero);
     // One subtile: logits of it into `d`, weights of the one before, whose logits `was`
     // holds, into `p`, and value product of the one before that, whose weights `pv` holds.
     auto subtile = [&](auto which, int t, f16_t &d, f16_t &was, u4_t (&p)[2], u4_t (&pv)[2]) INLINE {
       constexpr int S = decltype(which)::value;  // of the tile's two
-      const int j0 = (t_first + t) * TR + 32 * S;
+      const int j0 = tile(t) * TR + 32 * S;
       if constexpr (S == 1) __syncthreads();
       const u4_t *kt = k_tile(t), *kn = k_tile(t + S);
       auto ahead = [&](int k) INLINE {
@@ -580,7 +601,7 @@ struct SumArgs {
   const int4 *spans;  // of every 32 queries, or NULL (causal)
   float *sums;  // [batch, q_heads, T]
   int window;
-  int q_heads, kv_heads, units, nblk, run, T;
+  int q_heads, kv_heads, units, parts, nblk, run, T;
   float scale, cap;
   CapPoly poly;
 };
@@ -626,7 +647,7 @@ void prompt_colsum_kernel(SumArgs A) {
   const int wc = wave / WS, ws = wave % WS;
   const int G = A.q_heads / A.kv_heads, T = A.T, nsub = (T + 31) / 32;
   int hk, idx;
-  if (!block_unit(A.units, A.nblk * G, A.run, hk, idx)) return;
+  if (!block_of_unit(A.units, A.nblk * G, A.parts, A.run, hk, idx)) return;
   const int b = hk / A.kv_heads, kvh = hk % A.kv_heads, head = kvh * G + idx % G;
   const int j_base = idx / G * kKeys, j_wave = j_base + kWaveRows * wc;
   const int64_t row = ((int64_t)b * A.q_heads + head) * T;  // of lse and sums
@@ -841,6 +862,14 @@ unsigned grid_blocks(int units, int per_unit, int run) {
   return (unsigned)(8 * ((units + 7) / 8) * (((int64_t)per_unit + run - 1) / run * run));
 }
 
+// XCDs that a unit's blocks go to: the fewest that leave the eight evenly filled to an
+// eighth, so one unless there are few units.
+int unit_parts(int64_t units) {
+  int parts = 1;
+  while (parts < 8 && ((units * parts + 7) / 8 * 8 - units * parts) * 8 > units * parts) parts *= 2;
+  return parts;
+}
+
 template <class T>
 void copy3(T d[3], const T s[3]) { d[0] = s[0], d[1] = s[1], d[2] = s[2]; }
 
@@ -848,8 +877,10 @@ template <int NW>
 void launch_attention(PromptArgs &A, int G, bool cap, bool bias, hipStream_t st) {
   const int hw = std::min(G, NW), rows = kWaveQueries * (NW / hw), per_unit = (A.T + rows - 1) / rows * (G / hw);
   A.nblk = (A.T + rows - 1) / rows;
-  A.run = (int)std::min<int64_t>((int64_t)A.units * per_unit >= 4096 ? 32 : 4, per_unit);
-  const dim3 grid(grid_blocks(A.units, per_unit, A.run));
+  A.parts = unit_parts(A.units);
+  const int per_part = (per_unit + A.parts - 1) / A.parts;
+  A.run = (int)std::min<int64_t>((int64_t)A.units * per_unit >= 4096 ? 32 : 4, per_part);
+  const dim3 grid(grid_blocks(A.units * A.parts, per_part, A.run));
   auto kernel = cap ? (bias ? prompt_attention_kernel<true, true, NW> : prompt_attention_kernel<true, false, NW>)
                     : (bias ? prompt_attention_kernel<false, true, NW> : prompt_attention_kernel<false, false, NW>);
   hipLaunchKernelGGL(kernel, grid, dim3(64 * NW), 0, st, A);
@@ -947,9 +978,10 @@ extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rul
   const int share = n1 >= 768 ? 1 : n1 >= 192 ? 2 : 4;
   const int keys = kWaveRows * 4 / share;
   A.nblk = (p->tokens + keys - 1) / keys;
-  const int per_unit = A.nblk * G;
-  A.run = std::min(n1 >= 4096 ? 32 : 4, per_unit);
-  const dim3 grid(grid_blocks(A.units, per_unit, A.run));
+  A.parts = unit_parts(A.units);
+  const int per_part = (A.nblk * G + A.parts - 1) / A.parts;
+  A.run = std::min(n1 >= 4096 ? 32 : 4, per_part);
+  const dim3 grid(grid_blocks(A.units * A.parts, per_part, A.run));
   if (share == 1)
     launch_colsum<1>(A, grid, st);
   else if (share == 2)
