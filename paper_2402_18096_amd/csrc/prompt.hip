@@ -335,10 +335,29 @@ void prompt_attention_kernel(PromptArgs A) {
     };
     // final scores of a subtile of which not every query sees every key
     auto edge = [&](f16_t &d, int j0) INLINE {
+      if (j0 >= own_hi || j0 + 32 <= own_lo) {
+        d = splat(hidden_score<CAP>());
+        return;
+      }
+      if constexpr (CAP) {
+        float big = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(d[r]));
+        Coef c;
+        c.base = 0.0f;
+        c.p = A.poly;
+        if (__ballot(!(big < c.p.limit)) == 0) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) d[r] = term<true, false>(d[r], r, c);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) d[r] = tanh_fine(d[r] * A.scale) * A.cap;
+        }
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = j0 + tile_row(r);
-        float s = CAP ? tanh_fine(d[r] * A.scale) * A.cap : d[r] * A.scale;
+        float s = CAP ? d[r] : d[r] * A.scale;
         if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own - j), s);
         if constexpr (CAP) s = s < kLowest ? kLowest : s;
         d[r] = j >= lo && j < hi ? s : hidden_score<CAP>();
@@ -512,7 +531,12 @@ void prompt_attention_kernel(PromptArgs A) {
       const bool is_full = full(j0), ok = fine(ts);
       // (one branch, rarely taken, for all that is not plain)
       if (__builtin_expect(!ok || !is_full || !was_full, false)) {
-        if (!ok) raise(was, was_full, j_was, ts, p);
+        if (S == 0 && t == own_first) {  // nothing came before: m - m is not a number
+          ts = 0.0f;
+          p[0] = p[1] = u4_t{0, 0, 0, 0};
+        } else if (!ok) {
+          raise(was, was_full, j_was, ts, p);
+        }
         if (!is_full) edge(d, j0);
         if (!(j_was >= full_lo && j_was + 32 <= full_hi) && clean()) poison(v_was, p);
       }
