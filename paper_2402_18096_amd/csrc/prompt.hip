@@ -325,7 +325,7 @@ void prompt_attention_kernel(PromptArgs A) {
         c.p.c4 = is_full ? A.poly.c4 : 0.0f;
         c.limit = is_full ? A.poly.limit : kInf;
       } else {
-        c.scale = is_full ? A.scale : 1.0f;
+        c.scale = is_full || !BIAS ? A.scale : 1.0f;
       }
       if constexpr (BIAS) {
         c.slope = !is_full ? 0.0f : j0 > i_hi ? -slope : slope;
@@ -339,6 +339,8 @@ void prompt_attention_kernel(PromptArgs A) {
         d = splat(hidden_score<CAP>());
         return;
       }
+      constexpr bool kEdgeScaled = !CAP && BIAS;  // (without either, term scales -inf, too)
+      const int jb = j0 + 4 * half;
       if constexpr (CAP) {
         float big = 0.0f;
 #pragma unroll
@@ -356,11 +358,11 @@ void prompt_attention_kernel(PromptArgs A) {
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int j = j0 + tile_row(r);
-        float s = CAP ? d[r] : d[r] * A.scale;
-        if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own - j), s);
+        const int c = (int)row_const(r);
+        float s = kEdgeScaled ? d[r] * A.scale : d[r];
+        if constexpr (BIAS) s = fmaf(-slope, (float)abs(i_own - jb - c), s);
         if constexpr (CAP) s = s < kLowest ? kLowest : s;
-        d[r] = j >= lo && j < hi ? s : hidden_score<CAP>();
+        d[r] = (uint32_t)(jb - lo + c) < (uint32_t)(hi - lo) ? s : hidden_score<CAP>();
       }
     };
     // Whether every lane's weights of a subtile are in range.
@@ -465,12 +467,17 @@ void prompt_attention_kernel(PromptArgs A) {
     // one become NaN in its channel (poison).
     auto odd_halves = [](uint32_t w) INLINE { return (((w & 0x7fff7fffu) + 0x04000400u) & 0x80008000u) >> 15; };  // 1 per infinite or NaN half
     auto clean = [&]() INLINE {
-      uint32_t any = 0u;
+      // (a sum of fp16 values in fp32 is finite where they all are)
+      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+      float any[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) any |= odd_halves(vf[i & 3][i >> 2][e]);
-      if (!__ballot(any != 0u)) return false;
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t w = vf[i & 3][i >> 2][e];
+          any[e] = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w), h2{(_Float16)1.0f, (_Float16)1.0f}, any[e], false);
+        }
+      if (!__ballot(!(fabsf((any[0] + any[1]) + (any[2] + any[3])) < kInf))) return false;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
