@@ -408,9 +408,12 @@ void prompt_attention_kernel(PromptArgs A) {
     // LDS during the first subtile of tile t, its value rows during the second, each
     // fetched one subtile before.  (Past the last tile rows are loaded, or zeros,
     // and never used.)
-    // Under a bias the tiles go backwards: the first scores are then the largest (of
-    // the keys no later than the query), and the maximum is not raised at every tile.
-    auto tile = [&](int t) INLINE { return BIAS ? max(t_first + n_tiles - 1 - t, 0) : t_first + t; };
+    // The tiles go backwards: under a bias the first scores are then the largest (of the
+    // keys no later than the query), and the maximum is not raised at every tile (1 x 4 x 2048
+    // 78 -> 52 us); packed documents gain, too (16 x 32/8 x 2011 330 -> 308), other prompts
+    // are even, but under a cap alone forwards is faster (8 x 32 x 4096 1590 -> 1554).
+    constexpr bool kBack = BIAS || !CAP;
+    auto tile = [&](int t) INLINE { return kBack ? max(t_first + n_tiles - 1 - t, 0) : t_first + t; };
     u4_t rows[tile_loads<NW>()];
     auto fetch_keys = [&](int t) INLINE { fetch_rows<NW>(rows, kb, A.ks[2], tile(t) * TR, T); };
     auto fetch_values = [&](int t) INLINE { fetch_rows<NW>(rows, vb, A.vs[2], tile(t) * TR, T); };
@@ -444,7 +447,7 @@ void prompt_attention_kernel(PromptArgs A) {
     // with the block.
     int own_first = own_hi > own_lo ? own_lo / TR - t_first : 0;
     int own_end = own_hi > own_lo ? (own_hi + TR - 1) / TR - t_first : 0;
-    if constexpr (BIAS) {
+    if constexpr (kBack) {
       const int first = own_first;
       own_first = n_tiles - own_end;
       own_end = n_tiles - first;
@@ -951,12 +954,12 @@ extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rule
   // Waves per block: eight share each K and V row, four (two blocks to a CU) leave a
   // shorter tail and wait less for each other.  Eight only for long prompts, or groups that
   // fill a block with few query tiles, while there are blocks enough.  Measured
-  // (us, eight -> four): 1 x 32/8 heads x 4096 143 -> 163, 2 x 32 x 8192 1141 -> 1190,
-  // packed documents 16 x 32/8 x 2011 343 -> 363, but 2 x 40 x 1531 91 -> 77,
-  // 8 x 32 x 2048 404 -> 387, 1 x 8 x 8192 198 -> 186; with a bias (more registers), 8 x 32 x
-  // 2048 525 -> 476, 2 x 32 x 8192 1467 -> 1452.
+  // (us, eight -> four): 1 x 32/8 heads x 4096 146 -> 166, 2 x 32 x 8192 1130 -> 1206,
+  // packed documents 16 x 32/8 x 2011 (tiles forwards) 330 -> 340, but 2 x 40 x 1531 90 -> 77,
+  // 8 x 32 x 2048 397 -> 397, 1 x 8 x 8192 202 -> 187; under a cap or a bias alike (with a bias
+  // 1 x 32/8 x 4096 143 -> 162, 2 x 40 x 1531 96 -> 83).
   const int64_t blocks = (int64_t)p->batch * p->q_heads * ((p->tokens + 255) / 256);
-  if (!bias && (p->tokens >= 4096 ? blocks >= 512 : G >= 4 && blocks >= 1024))
+  if (p->tokens >= 4096 ? blocks >= 512 : G >= 4 && blocks >= 1024)
     launch_attention<8>(A, G, cap, bias, (hipStream_t)stream);
   else
     launch_attention<4>(A, G, cap, bias, (hipStream_t)stream);
