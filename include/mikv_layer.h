@@ -85,7 +85,8 @@ typedef struct mikv_heads {
  * Rows that are 16-byte aligned, with rot_dim a multiple of 16, are read
  * and written 16 bytes at a time; others work, more slowly.
  * Errors: INVALID_ARG (NULL, counts < 1, rot_dim odd or outside 2 .. 128, x or y not
- * aligned to its type, unknown types or pairs of types, in place between two types);
+ * aligned to its type, unknown types or pairs of types, in place between two types or
+ * strides, rows of y that share memory: a stride of 0);
  * UNSUPPORTED (head_dim != 128, over 2^24 tokens in all, over 2^16 heads).
  */
 int mikv_rotary(const mikv_heads *tensors, int32_t n, int32_t batch, int32_t tokens, int32_t head_dim, int32_t x_type,
@@ -122,7 +123,7 @@ typedef struct mikv_score_rules {
  *   prefix    int32 [batch] or NULL: leading positions that every query of the same document sees;
  *   window    0: none;
  *   begin, end int32 [batch, tokens] (outputs).
- * Errors: INVALID_ARG (NULL outputs, counts < 1, window < 0).
+ * Errors: INVALID_ARG (NULL outputs, counts < 1, window < 0); UNSUPPORTED (over 2^30 tokens).
  */
 int mikv_mask_spans(const int32_t *documents, const int32_t *prefix, int32_t batch, int32_t tokens, int32_t window,
                     int32_t *begin, int32_t *end, void *stream);
@@ -142,7 +143,7 @@ typedef struct mikv_prompt {
  * Products are fp16 with fp32 sums on the matrix cores; scores, maxima, sums and
  * the output's accumulation are fp32, the weights of the value product fp16.
  *   rules  HOST pointer, or NULL: causal, no cap, no bias;
- *   out    fp16 [batch, q_heads, tokens, 128] through out_stride (as q's);
+ *   out    fp16 [batch, q_heads, tokens, 128] through out_stride (as q's, no stride 0);
  *   lse    fp32 [batch, q_heads, tokens] or NULL: natural log of the sum of exp(s).
  * Errors: INVALID_ARG (NULL, counts < 1, q_heads % kv_heads, alignment, strides, scale, cap, window);
  * UNSUPPORTED (head_dim, query heads per KV head, a token stride over 2^22, grids over 2^31).

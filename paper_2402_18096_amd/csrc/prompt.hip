@@ -827,10 +827,10 @@ void prompt_colsum_kernel(SumArgs A) {
   if (kj < T) A.sums[row + kj] = v;
 }
 
-__global__ __launch_bounds__(256) void sum_heads_kernel(const float *sums, int G, int T, float *scores) {
+__global__ __launch_bounds__(256) void sum_heads_kernel(const float *sums, int units, int G, int T, float *scores) {
   const int j = blockIdx.x * 256 + threadIdx.x;
   const int64_t hk = (int64_t)blockIdx.z * 65535 + blockIdx.y;
-  if (j >= T) return;
+  if (j >= T || hk >= units) return;
   const float *p = sums + hk * G * T + j;
   float v = p[0];
   for (int g = 1; g < G; ++g) v += p[(int64_t)g * T];
@@ -941,6 +941,8 @@ extern "C" int mikv_prompt_attention(const mikv_prompt *p, const mikv_score_rule
   if (int e = check_rows(who, "v", p->v, p->v_stride)) return e;
   if (!out_stride) return set_error(MIKV_ERR_INVALID_ARG, "%s: out_stride is NULL", who);
   if (int e = check_rows(who, "out", out, out_stride)) return e;
+  if ((p->batch > 1 && !out_stride[0]) || (p->q_heads > 1 && !out_stride[1]) || (p->tokens > 1 && !out_stride[2]))
+    return set_error(MIKV_ERR_INVALID_ARG, "%s: the output's rows share memory (stride 0)", who);
   if ((uintptr_t)lse % 4) return set_error(MIKV_ERR_INVALID_ARG, "%s: misaligned lse", who);
   PromptArgs A{};
   A.q = p->q, A.k = p->k, A.v = p->v, A.out = out, A.lse = lse;
@@ -1024,6 +1026,6 @@ extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rul
     launch_colsum<4>(A, grid, st);
   if (G > 1)
     hipLaunchKernelGGL(sum_heads_kernel, dim3((p->tokens + 255) / 256, std::min(65535, A.units), (A.units + 65534) / 65535),
-                       dim3(256), 0, st, (const float *)A.sums, G, p->tokens, scores);
+                       dim3(256), 0, st, (const float *)A.sums, A.units, G, p->tokens, scores);
   return check_launch(who);
 }

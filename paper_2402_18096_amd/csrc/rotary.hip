@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotArgs A) {
     const int64_t pos = A.positions ? A.positions[row] : (int64_t)A.pos0 + t;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-      const int32_t phase = (int32_t)((uint64_t)(pos * (int64_t)A.freq[W * c + i]) >> 32);
+      const int32_t phase = (int32_t)((uint64_t)pos * A.freq[W * c + i] >> 32);
       sincospif((float)phase * 0x1p-31f, &sn[i], &cs[i]);
       sn[i] *= A.magnitude;
       cs[i] *= A.magnitude;
@@ -244,6 +244,8 @@ extern "C" int mikv_rotary(const mikv_heads *tensors, int32_t n, int32_t batch, 
     R.yb = h.y_stride[0], R.yh = h.y_stride[1], R.yt = h.y_stride[2];
     if (h.x == h.y && ((batch > 1 && R.xb != R.yb) || (h.heads > 1 && R.xh != R.yh) || (tokens > 1 && R.xt != R.yt)))
       return set_error(MIKV_ERR_INVALID_ARG, "mikv_rotary: in place needs the same strides");
+    if ((batch > 1 && !R.yb) || (h.heads > 1 && !R.yh) || (tokens > 1 && !R.yt))
+      return set_error(MIKV_ERR_INVALID_ARG, "mikv_rotary: the output's rows share memory (stride 0)");
     R.heads = h.heads;
     R.rotate = h.rotate;
     heads += h.heads;

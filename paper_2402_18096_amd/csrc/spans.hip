@@ -83,6 +83,7 @@ extern "C" int mikv_mask_spans(const int32_t *documents, const int32_t *prefix, 
   if (!begin || !end) return set_error(MIKV_ERR_INVALID_ARG, "mikv_mask_spans: NULL output");
   if (batch < 1 || tokens < 1 || window < 0)
     return set_error(MIKV_ERR_INVALID_ARG, "mikv_mask_spans: batch and tokens >= 1, window >= 0 expected");
+  if (tokens > 1 << 30) return set_error(MIKV_ERR_UNSUPPORTED, "mikv_mask_spans: over 2^30 tokens");
   if (((uintptr_t)documents | (uintptr_t)prefix | (uintptr_t)begin | (uintptr_t)end) % 4)
     return set_error(MIKV_ERR_INVALID_ARG, "mikv_mask_spans: misaligned pointer");
   hipLaunchKernelGGL(mask_spans_kernel, dim3(batch), dim3(kSpanBlock), 0, (hipStream_t)stream, documents, prefix, tokens,

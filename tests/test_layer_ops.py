@@ -642,6 +642,33 @@ def test_binding_refusals():
         mikv.mikv_mask_spans(torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, 3, dtype=torch.int32))
 
 
+def test_outputs_whose_rows_share_memory_are_refused():
+    p = ctypes.byref(_prompt_desc())
+    for stride in ([8192 * 4, 0, 128], [8192 * 4, 8192, 0]):
+        assert _code("mikv_prompt_attention", p, None, 0x1000, (ctypes.c_int64 * 3)(*stride), None, None) == 1
+    h = (mikv.Heads * 1)()
+    h[0].x, h[0].y, h[0].heads, h[0].rotate = 0x1000, 0x2000, 4, 1
+    for stride in ([0, 512, 128], [2048, 0, 128], [2048, 512, 0]):
+        h[0].x_stride[:], h[0].y_stride[:] = [2048, 512, 128], stride
+        assert _code("mikv_rotary", h, 1, 2, 4, 128, 0, 0, None, 0, 0x1000, 128, 0, 1.0, None) == 1
+    assert _code("mikv_mask_spans", None, None, 1, (1 << 30) + 1, 0, 0x1000, 0x1000, None) == 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hkv", [(2, 1), (1, 1)])
+def test_prompts_of_more_heads_than_a_grid_dimension(Hq, Hkv):
+    # one token: it sees itself alone, so out = v, lse = its score, importance = the heads of its group
+    B = 70000
+    q, k, v = _prompt(B, Hq, Hkv, 1, seed=1)
+    out, lse = _run_attention(q, k, v, mikv.ScoreRules(window=1))
+    assert torch.equal(out, v.expand(B, Hkv, 1, D).repeat_interleave(Hq // Hkv, 1))
+    scores = torch.full((B + 8, Hkv, 1), -1.0, device="cuda")
+    mikv.mikv_prompt_importance(q, k, lse, scores[:B], mikv.ScoreRules(window=1))
+    # exp2(s - lse) of the same fp32 score: lse in and out of log2 units and the difference are three roundings of
+    # numbers below 16, 2^-21 each, two exponentials half a step or a whole one off: under 4e-6 for two heads
+    assert float((scores[:B] - Hq // Hkv).abs().max()) <= 4e-6 and bool((scores[B:] == -1.0).all())
+
+
 def test_packed_descriptors_have_the_mirrors_layout():
     h = mikv.Heads.from_buffer_copy(mikv._HEADS.pack(16, 32, 1, 2, 3, 4, 5, 6, 7, 1))
     assert (h.x, h.y, list(h.x_stride), list(h.y_stride), h.heads, h.rotate) == (16, 32, [1, 2, 3], [4, 5, 6], 7, 1)
