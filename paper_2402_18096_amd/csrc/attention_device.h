@@ -425,6 +425,31 @@ __device__ inline void load_seg_rows(Rows<BITS, CPL> &r, rsrc_t rk, rsrc_t rv, r
   }
 }
 
+// RULES: the iterations [lo, hi) of PER tokens outside of which slots [start, end) of a
+// pool hold no token from position `begin` on.  The pools keep the prompt's order, so
+// whole chunks are left out of a windowed or padded cache; looking costs a trip to memory, so
+// only where at least a quarter of the positions is hidden (16 x 32/8 x 16384, fp16 over
+// INT2, the last 4096 positions: 83 us without it, 60 with).
+template <int PER>
+__device__ inline void visible_range(const RuleArgs &R, rsrc_t rpos, int begin, int start, int end, int &lo, int &hi) {
+  if (begin == 0 || (int64_t)begin * 4 < R.last) return;
+  int first = end, last = start - 1;
+  for (int s = start + (int)(threadIdx.x & 63); s < end; s += 64)
+    if ((int)__builtin_amdgcn_raw_buffer_load_b32(rpos, (uint32_t)s * 4u, 0, 0) >= begin) {
+      first = min(first, s);
+      last = s;
+    }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    first = min(first, __shfl_xor(first, o, 64));
+    last = max(last, __shfl_xor(last, o, 64));
+  }
+  first = __builtin_amdgcn_readfirstlane(first);
+  last = __builtin_amdgcn_readfirstlane(last);
+  lo = last < first ? 0 : (first - start) / PER;
+  hi = last < first ? 0 : (last - start) / PER + 1;
+}
+
 // KPC: retained keys quantized per channel over 64-position blocks
 // (Appendix C).  The key's "parameter" word is then its position; a lane
 // keeps q_c * alpha_c (times the code class factor) and sum_c q_c beta_c for
@@ -516,7 +541,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
       for (int i = 0; i < Rows<BITS, CPL>::KW; ++i) out[i] = raw[i];
     }
   };
-  const int n_iter = end > start ? (end - start + kPerIter - 1) / kPerIter : 0;
+  int n_iter = end > start ? (end - start + kPerIter - 1) / kPerIter : 0;
   const int first = start + wave * TPW * UNROLL + tsub;  // this lane's token in iteration 0, u = 0
   const int g_lane = (part * CPL) / A.group;
   // Buffer resources over this head's occupied slots; a lane's offset is
@@ -528,6 +553,17 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
   const rsrc_t rvp = make_rsrc(Q ? (const void *)vpb : (const void *)vb, Q ? (uint32_t)n_pool * ng * 4u : 0u);
   const rsrc_t rpos = make_rsrc(RULES ? (const void *)((is_hi ? A.hi_pos : A.lo_pos) + (int64_t)h * cap) : (const void *)kb,
                                 RULES && rule_positions(A.rules) ? (uint32_t)n_pool * 4u : 0u);
+  int begin = 0, it_end = n_iter;  // first visible position; end of the iterations
+  if constexpr (RULES) {
+    begin = rule_begin(A.rules, b);
+    int it_begin = 0;
+    visible_range<kPerIter>(A.rules, rpos, begin, start, end, it_begin, it_end);
+    if (it_end - it_begin < n_iter) {
+      for (int i = 0; i < G; ++i)
+        for (int j = lane; j < end - start; j += 64) s_lds[i * max_chunk(G) + j] = kNegInf;
+    }
+    n_iter = it_end - it_begin;
+  }
   const uint32_t lane_tok = (uint32_t)(start + wave * TPW * UNROLL + tsub);
   const uint32_t off_row0 = lane_tok * (uint32_t)kRow + seg_off;
   const uint32_t off_par0 = (lane_tok * (uint32_t)ng + (uint32_t)g_lane) * 4u;
@@ -537,7 +573,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
   // zero without a memory access, so a load needs no branch around it.
   const rsrc_t r_none = make_rsrc(kb, 0u);
   auto load_part = [&](auto which, Rows<BITS, CPL>(&r)[UNROLL], int it, bool live = true) {
-    if constexpr (RULES) it = n_iter - 1 - it;
+    if constexpr (RULES) it = it_end - 1 - it;
     const uint32_t orow = off_row0 + (uint32_t)(it * kPerIter) * (uint32_t)kRow;
     const uint32_t opar = off_par0 + (uint32_t)(it * kPerIter) * (uint32_t)ng * 4u;
     const uint32_t okp = KPC ? off_kp0 + (uint32_t)(it * kPerIter) * 4u : opar;
@@ -617,10 +653,8 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
   }
   const float s2scale_q = Q ? __builtin_ldexpf(s2scale, 24 - qshift) : s2scale;
   float arg_scale = 0.0f, slope2 = 0.0f;
-  int begin = 0;
   if constexpr (RULES) {
     arg_scale = Q ? __builtin_ldexpf(A.rules.cap_scale, 24 - qshift) : A.rules.cap_scale;
-    begin = rule_begin(A.rules, b);
     if (A.rules.slopes) slope2 = A.rules.slopes[kvh * G + own] * kLog2e;
   }
 #pragma unroll
@@ -706,7 +740,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
   // Scores of one iteration (and the lazy running-max update).
   auto proc_k = [&](Rows<BITS, CPL>(&cur)[UNROLL], int it) {
     uint64_t raise = 0;  // lanes whose score passes the lazy threshold (a ballot per token)
-    if constexpr (RULES) it = n_iter - 1 - it;
+    if constexpr (RULES) it = it_end - 1 - it;
     const int rem = end - it * kPerIter;  // wave-uniform: a token is valid when first + u * TPW < rem
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
@@ -1027,7 +1061,7 @@ __device__ void attn_chunk_int2(const AttnArgs &A, int h, int chunk, int rec_chu
   const int n_pool = __builtin_amdgcn_readfirstlane(A.n_lo[h]);
   const int start = chunk * A.chunk_lo;
   const int end = min(start + A.chunk_lo, n_pool);
-  const int n_iter = end > start ? (end - start + kItTok - 1) / kItTok : 0;
+  int n_iter = end > start ? (end - start + kItTok - 1) / kItTok : 0;
   float *scores = A.scores_lo;
 
   const rsrc_t rk = make_rsrc(A.lo_k + (int64_t)h * cap * 32, (uint32_t)n_pool * 32u);
@@ -1036,6 +1070,18 @@ __device__ void attn_chunk_int2(const AttnArgs &A, int h, int chunk, int rec_chu
   const rsrc_t rvp = make_rsrc(A.lo_vp + (int64_t)h * cap * NG, (uint32_t)n_pool * NG * 4u);
   const rsrc_t rpos = make_rsrc(RULES ? (const void *)(A.lo_pos + (int64_t)h * cap) : (const void *)A.lo_k,
                                 RULES && rule_positions(A.rules) ? (uint32_t)n_pool * 4u : 0u);
+
+  int begin = 0, it_end = n_iter;
+  if constexpr (RULES) {
+    begin = rule_begin(A.rules, b);
+    int it_begin = 0;
+    visible_range<kItTok>(A.rules, rpos, begin, start, end, it_begin, it_end);
+    if (it_end - it_begin < n_iter && scores) {
+      for (int i = 0; i < G; ++i)
+        for (int j = lane; j < end - start; j += 64) s_lds[i * max_chunk(G) + j] = kNegInf;
+    }
+    n_iter = it_end - it_begin;
+  }
 
   // One iteration's loads: key codes and parameter rows of the four key
   // tiles (the lane's value groups only), value codes of the two tiles.
@@ -1051,7 +1097,7 @@ __device__ void attn_chunk_int2(const AttnArgs &A, int h, int chunk, int rec_chu
   // descriptor (zero, no memory access), so no branch is needed around it.
   const rsrc_t r_none = make_rsrc(A.lo_k, 0u);
   auto load = [&](Ld &d, int it, bool keys, bool vals, bool live) {
-    const uint32_t t0 = (uint32_t)(start + (RULES ? n_iter - 1 - it : it) * kItTok);
+    const uint32_t t0 = (uint32_t)(start + (RULES ? it_end - 1 - it : it) * kItTok);
     const rsrc_t ak = live ? rk : r_none, av = live ? rv : r_none;
     const rsrc_t akp = live ? rkp : r_none, avp = live ? rvp : r_none;
 #pragma unroll
@@ -1157,10 +1203,8 @@ __device__ void attn_chunk_int2(const AttnArgs &A, int h, int chunk, int rec_chu
   const int qshift = qm * 256.0f < 60000.0f ? 6 : qm * 64.0f < 60000.0f ? 4 : qm * 16.0f < 60000.0f ? 2 : 0;
   const float s2scale_q = __builtin_ldexpf(A.scale * kLog2e, 16 - qshift);
   float arg_scale = 0.0f, slope2[RULES ? NSET : 1];  // slopes of the lane's own queries
-  int begin = 0;
   if constexpr (RULES) {
     arg_scale = __builtin_ldexpf(A.rules.cap_scale, 16 - qshift);
-    begin = rule_begin(A.rules, b);
 #pragma unroll
     for (int st = 0; st < NSET; ++st) slope2[st] = A.rules.slopes ? A.rules.slopes[kvh * G + qs + 4 * st] * kLog2e : 0.0f;
   }
@@ -1244,7 +1288,7 @@ __device__ void attn_chunk_int2(const AttnArgs &A, int h, int chunk, int rec_chu
   // loaded once the scores are done, its values once the value MFMAs are.
   for (int it = 0; it < n_iter; ++it) {
     const bool live = it + 1 < n_iter;
-    const int t0 = start + (RULES ? n_iter - 1 - it : it) * kItTok;
+    const int t0 = start + (RULES ? it_end - 1 - it : it) * kItTok;
     // --- scores of the four key tiles
     float s2[kKT][NSET];
     uint64_t raise = 0;
