@@ -1016,7 +1016,10 @@ extern "C" int mikv_prompt_importance(const mikv_prompt *p, const mikv_score_rul
   A.nblk = (p->tokens + keys - 1) / keys;
   A.parts = unit_parts(A.units);
   const int per_part = (A.nblk * G + A.parts - 1) / A.parts;
-  A.run = std::min(n1 >= 4096 ? 32 : 4, per_part);
+  // Runs of one key block's heads, which read the same keys: longer ones put long blocks at
+  // the grid's end (8 x 32 x 2048: runs of one 205 us, of 32 267; 2 x 32 x 8192 630 and 701;
+  // packed documents 8 x 32/8 x 4096: of one 517, of four 412, of 32 427).
+  A.run = std::min(G, per_part);
   const dim3 grid(grid_blocks(A.units * A.parts, per_part, A.run));
   if (share == 1)
     launch_colsum<1>(A, grid, st);
