@@ -326,6 +326,42 @@ def test_prompt_attention_masks(T, Hq, Hkv, docs, prefix, window, cap, bias):
 
 
 @gpu
+@pytest.mark.parametrize("Hq,Hkv,T", [(64, 8, 65), (32, 8, 385)])
+@pytest.mark.parametrize("docs", [None, "few"])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (20.0, False), (0.0, True), (20.0, True)])
+def test_prompts_of_a_full_grid(Hq, Hkv, T, docs, cap, bias):
+    """Batches that fill the grid, where a block's eight waves share the rows; a few sequences are checked."""
+    B = 16
+    ids = _documents(docs, B, T, np.random.default_rng(T))
+    q, k, v = _prompt(B, Hq, Hkv, T, seed=T, packed=True)
+    begin, end = _spans(B, T, ids, None, 0)
+    slopes = _slopes(Hq) if bias else None
+    rules = mikv.ScoreRules(cap, slopes, begin, end)
+    out, lse = _run_attention(q, k, v, rules)
+    scores = torch.full((B, Hkv, T), float("nan"), device="cuda")
+    mikv.mikv_prompt_importance(q, k, lse, scores, rules)
+    seen = _seen(B, T, ids, None, 0)
+    for b in (0, B - 1):
+        _check_attention(q[b:b + 1], k[b:b + 1], v[b:b + 1], out[b:b + 1], lse[b:b + 1], seen[b:b + 1], cap, slopes)
+        _check_importance(q[b:b + 1], k[b:b + 1], lse[b:b + 1], scores[b:b + 1], seen[b:b + 1], cap, slopes)
+
+
+@gpu
+@pytest.mark.parametrize("B,Hq,Hkv", [(1, 1, 1), (1, 4, 2), (3, 8, 1), (1, 5, 5), (2, 6, 6), (11, 4, 2)])
+def test_prompts_of_few_heads(B, Hq, Hkv):
+    """Heads that do not fill the eight dies evenly share their blocks out (or not): every row is written once."""
+    T = 700
+    q, k, v = _prompt(B, Hq, Hkv, T, seed=B)
+    out, lse = _run_attention(q, k, v, None)
+    scores = torch.full((B, Hkv, T), float("nan"), device="cuda")
+    mikv.mikv_prompt_importance(q, k, lse, scores)
+    b = B - 1
+    _check_attention(q[b:], k[b:], v[b:], out[b:], lse[b:], _seen(1, T))
+    _check_importance(q[b:], k[b:], lse[b:], scores[b:], _seen(1, T))
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(scores).all())
+
+
+@gpu
 def test_prompt_attention_any_interval():
     """begin and end of the caller's own, out of range, empty and ahead of the query among them."""
     T, Hq = 333, 4
