@@ -276,20 +276,6 @@ __device__ inline float token_sum(float v) {
   return v;
 }
 
-template <int CTRL>
-__device__ inline float dpp_mov(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
-}
-
-// Lanes whose number has bit `bit`, as a scalar mask (a compare would take a vector
-// instruction at every use).
-template <int BIT>
-__device__ inline bool lanes_with() {
-  return __builtin_amdgcn_inverse_ballot_w64(BIT == 1   ? 0xaaaaaaaaaaaaaaaaull
-                                             : BIT == 2 ? 0xccccccccccccccccull
-                                                        : 0xf0f0f0f0f0f0f0f0ull);
-}
-
 // token_sum of G values at once that leaves each lane only the sum of value
 // part % G: while a bit of `part` numbers values, a lane keeps the half that its bit names
 // and gives the other half away.  v[0] is the sum.

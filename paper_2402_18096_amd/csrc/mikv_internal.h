@@ -372,6 +372,16 @@ __device__ inline float dpp_mov(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
 
+// Lanes whose number has bit BIT (1, 2, 4 or 8), as a scalar mask (a compare would take a
+// vector instruction at every use).
+template <int BIT>
+__device__ inline bool lanes_with() {
+  return __builtin_amdgcn_inverse_ballot_w64(BIT == 1   ? 0xaaaaaaaaaaaaaaaaull
+                                             : BIT == 2 ? 0xccccccccccccccccull
+                                             : BIT == 4 ? 0xf0f0f0f0f0f0f0f0ull
+                                                        : 0xff00ff00ff00ff00ull);
+}
+
 __device__ inline float lane_value(float v, int lane) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }

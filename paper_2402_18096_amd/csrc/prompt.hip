@@ -665,6 +665,32 @@ __device__ inline int4 causal_span(int i0, int T) {
   return i0 >= T ? make_int4(T, 0, 0, 0) : make_int4(0, min(i0 + 32, T), 0, i0 + 31 < T ? i0 + 1 : 0);
 }
 
+// Sums of 32 values over each half of the wave: lane n of a half gets value n's.  The
+// lanes 16, 8, 4, 2 and 1 away exchange the halves of the values that the other one keeps:
+// 31 exchanges (a butterfly per value takes 160).
+template <int SPAN = 8>
+__device__ inline float own_sum16(float (&v)[32]) {
+  if constexpr (SPAN == 0) {
+    return v[0];
+  } else {
+    const bool up = lanes_with<SPAN>();
+#pragma unroll
+    for (int k = 0; k < SPAN; ++k)
+      v[k] = (up ? v[k + SPAN] : v[k]) +
+             dpp_mov<SPAN == 8 ? 0x140 : SPAN == 4 ? 0x141 : SPAN == 2 ? 0x4E : 0xB1>(up ? v[k] : v[k + SPAN]);
+    return own_sum16<SPAN / 2>(v);
+  }
+}
+__device__ inline float own_sum32(float (&v)[32]) {
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v[k]), __builtin_bit_cast(uint32_t, v[k + 16]), false, false);
+    const uint32_t x = r[0], y = r[1];
+    v[k] = __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y);
+  }
+  return own_sum16(v);
+}
+
 template <int WS>
 constexpr int sum_rows() { return WS == 4 ? 128 : 64; }
 
@@ -820,16 +846,12 @@ void prompt_colsum_kernel(SumArgs A) {
       commit(buf);
     }
   }
-  // over the tile's 32 query columns, then over the WS waves
+  // over the tile's 32 query columns, then over the WS waves: lane n of a half has the
+  // half's rows tile_row(n % 16) of the first (n < 16) or second 32 keys
+  float v32[32];
 #pragma unroll
-  for (int cb = 0; cb < 2; ++cb)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      float v = cs[cb][r];
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-      if (n == 0) s_sum[wave][32 * cb + tile_row(r)] = v;
-    }
+  for (int r = 0; r < 32; ++r) v32[r] = cs[r >> 4][r & 15];
+  s_sum[wave][32 * (n >> 4) + tile_row(n & 15)] = own_sum32(v32);
   __syncthreads();
   if (ws != 0) return;
   float v = s_sum[wave][lane];
