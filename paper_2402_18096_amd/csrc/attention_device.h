@@ -336,6 +336,16 @@ __device__ inline float sum_token_lanes(float v) {
   return v;
 }
 
+// A reduction over the lanes of the same number modulo G (1, 2, 4 or 8), in every lane.
+template <int G, class Op>
+__device__ inline float over_lanes(float v, Op op) {
+  if constexpr (G <= 1) v = op(v, dpp_mov<0xB1>(v));
+  if constexpr (G <= 2) v = op(v, dpp_mov<0x4E>(v));
+  if constexpr (G <= 4) v = op(v, dpp_mov<0x124>(v));
+  v = op(v, dpp_mov<0x128>(v));
+  return with_half(with_row(v, op), op);
+}
+
 // A 3-bit lane segment of 16 (8) channels is 48 (24) bits: two dwords are
 // loaded from the dword that holds its first bit and shifted (seg_shift) so
 // that the segment starts at bit 0.
@@ -794,9 +804,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
         float mx = s2[0][0], f[G];
 #pragma unroll
         for (int u = 1; u < UNROLL; ++u) mx = fmaxf(mx, s2[u][0]);
-#pragma unroll
-        for (int o = G; o < 64; o *= 2) mx = fmaxf(mx, __shfl_xor(mx, o, 64));  // over the lanes of this head
-        mx = fmaxf(mx, m2[0]);
+        mx = fmaxf(over_lanes<G>(mx, [](float x, float y) { return fmaxf(x, y); }), m2[0]);
         const float fo = m2[0] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m2[0] - mx);
         m2[0] = mx;
         l[0] *= fo;
@@ -939,9 +947,7 @@ __device__ void attn_chunk(const AttnArgs &A, int h, int chunk, int rec_chunk, b
     for (int c = 0; c < CPL; ++c) o[i][c] = sum_token_lanes<LPT>(o[i][c]);
   }
   if constexpr (RULES) {  // over the lanes of this lane's head, LPT / G of them per token
-#pragma unroll
-    for (int x = G; x < 64; x *= 2) l[0] += __shfl_xor(l[0], x, 64);
-    l[0] *= (float)G / LPT;
+    l[0] = over_lanes<G>(l[0], [](float x, float y) { return x + y; }) * ((float)G / LPT);
   }
   const int nc = A.nc_hi + A.nc_lo;
 #pragma unroll

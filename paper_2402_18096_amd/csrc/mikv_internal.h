@@ -372,6 +372,21 @@ __device__ inline float dpp_mov(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
 
+// op of a lane's value and the one 16, or 32, lanes away (one VALU instruction; a shuffle
+// through LDS takes a round trip of it).
+template <class Op>
+__device__ inline float with_row(float v, Op op) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  const uint32_t x = r[0], y = r[1];
+  return op(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
+}
+template <class Op>
+__device__ inline float with_half(float v, Op op) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+  const uint32_t x = r[0], y = r[1];
+  return op(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y));
+}
+
 // Lanes whose number has bit BIT (1, 2, 4 or 8), as a scalar mask (a compare would take a
 // vector instruction at every use).
 template <int BIT>

@@ -227,10 +227,14 @@ __device__ inline float other_half(float v) {
   return __builtin_bit_cast(float, (threadIdx.x & 32) ? r[0] : r[1]);
 }
 
+// Smallest of all lanes, as a scalar (DPP inside the rows of 16, as wave_max).
 __device__ inline int wave_min_int(int v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
-  return __builtin_amdgcn_readfirstlane(v);
+  v = min(v, __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true));
+  v = min(v, __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true));
+  v = min(v, __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true));
+  v = min(v, __builtin_amdgcn_mov_dpp(v, 0x140, 0xF, 0xF, true));
+  const int a = min(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16));
+  return min(a, min(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
 }
 __device__ inline int wave_max_int(int v) { return -wave_min_int(-v); }
 
@@ -727,8 +731,8 @@ void prompt_colsum_kernel(SumArgs A) {
       last = s;
     }
   }
-  first = min(wave_min_int(first), wave_min_int(__shfl_xor(first, 32, 64)));
-  last = max(wave_max_int(last), wave_max_int(__shfl_xor(last, 32, 64)));
+  first = wave_min_int(first);
+  last = wave_max_int(last);
   if (lane == 0) {
     s_range[wave][0] = first;
     s_range[wave][1] = last;
