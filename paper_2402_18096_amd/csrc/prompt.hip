@@ -414,10 +414,11 @@ void prompt_attention_kernel(PromptArgs A) {
     // and never used.)
     // The tiles go backwards: under a bias the first scores are then the largest (of the
     // keys no later than the query), and the maximum is not raised at every tile (1 x 4 x 2048
-    // 78 -> 52 us); packed documents gain, too (16 x 32/8 x 2011 330 -> 308), other prompts
-    // are even, but under a cap alone forwards is faster (8 x 32 x 4096 1590 -> 1554).
-    constexpr bool kBack = BIAS || !CAP;
-    auto tile = [&](int t) INLINE { return kBack ? max(t_first + n_tiles - 1 - t, 0) : t_first + t; };
+    // 78 -> 52 us); packed documents gain, too (16 x 32/8 x 2011 330 -> 308, under a cap 454 ->
+    // 402, 8 x 32 x 4096 1004 -> 810), other prompts are even, but under a cap alone forwards is
+    // a percent faster (8 x 32 x 4096 1612 -> 1593).
+    const bool back = BIAS || !CAP || A.begin || A.end;
+    auto tile = [&](int t) INLINE { return back ? max(t_first + n_tiles - 1 - t, 0) : t_first + t; };
     u4_t rows[tile_loads<NW>()];
     auto fetch_keys = [&](int t) INLINE { fetch_rows<NW>(rows, kb, A.ks[2], tile(t) * TR, T); };
     auto fetch_values = [&](int t) INLINE { fetch_rows<NW>(rows, vb, A.vs[2], tile(t) * TR, T); };
@@ -451,7 +452,7 @@ void prompt_attention_kernel(PromptArgs A) {
     // with the block.
     int own_first = own_hi > own_lo ? own_lo / TR - t_first : 0;
     int own_end = own_hi > own_lo ? (own_hi + TR - 1) / TR - t_first : 0;
-    if constexpr (kBack) {
+    if (back) {
       const int first = own_first;
       own_first = n_tiles - own_end;
       own_end = n_tiles - first;
