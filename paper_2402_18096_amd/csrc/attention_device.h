@@ -428,7 +428,7 @@ __device__ inline void load_seg_rows(Rows<BITS, CPL> &r, rsrc_t rk, rsrc_t rv, r
 // INT2, the last 4096 positions: 83 us without it, 60 with).
 template <int PER>
 __device__ inline void visible_range(const RuleArgs &R, rsrc_t rpos, int begin, int start, int end, int &lo, int &hi) {
-  if (begin == 0 || (int64_t)begin * 4 < R.last) return;
+  if (end <= start || begin == 0 || (int64_t)begin * 4 < R.last) return;  // (an empty chunk ends before it starts)
   int first = end, last = start - 1;
   for (int s = start + (int)(threadIdx.x & 63); s < end; s += 64)
     if ((int)__builtin_amdgcn_raw_buffer_load_b32(rpos, (uint32_t)s * 4u, 0, 0) >= begin) {

@@ -159,6 +159,36 @@ def test_hidden_tokens_hold_anything(hi, lo, G, bad):
 
 
 @gpu
+@pytest.mark.parametrize("hi,lo,G", [(16, 2, 1), (16, 2, 2), (16, 2, 8), (16, 3, 1), (8, 4, 4), (4, 2, 2), (16, 8, 8), (16, 0, 4)])
+def test_window_over_chunks(hi, lo, G):
+    """A window that hides whole chunks of both pools, in a cache of far more capacity than tokens (empty chunks): the cache
+    of the window's tokens alone, but for the order of the sums."""
+    T, W, cap = 3001, 403, 9000
+    g = torch.Generator(device="cuda").manual_seed(hi + lo)
+    k, v = (torch.randn(2, 2, T, 128, device="cuda", generator=g).half() for _ in range(2))
+    q = torch.randn(2, 2 * G, 128, device="cuda", generator=g).half()
+    mask = (torch.rand(2, 2, T, device="cuda", generator=g) < 0.3).to(torch.uint8)
+    got = []
+    for first, rules in ((0, mikv.ScoreRules(window=W)), (T - W, mikv.ScoreRules(window=cap))):
+        n = T - first
+        c = mikv.MikvCache(2, 2 * G, 2, 32, hi, lo, cap, cap, cap)
+        mikv.mikv_quantize_kv(c, k[:, :, first:].contiguous(), v[:, :, first:].contiguous(), 0, None, mask[:, :, first:].contiguous())
+        out = torch.empty(2, 2 * G, 128, device="cuda")
+        ph = torch.zeros(2, 2 * G, c.cap_hi, device="cuda")
+        pl = torch.zeros(2, 2 * G, c.cap_lo, device="cuda") if lo else None
+        mikv.mikv_decode_attention_scored(c, n, q, out, ph, pl, rules)
+        probs = torch.empty(2, 2 * G, n, device="cuda")
+        mikv.mikv_probs_by_position(c, n, ph, pl, probs)
+        got.append((out, probs))
+    (out, probs), (want, p) = got
+    assert bool((probs[..., :T - W] == 0).all())
+    # sums of at most W terms in another order, exponentials and split weights against another maximum: 2^-23 each
+    tol = (W + 16) * 2.0 ** -23
+    assert bool(((probs[..., T - W:] - p).abs() <= tol * p).all())
+    assert float((out - want).abs().max()) <= tol * float(v.abs().max())
+
+
+@gpu
 def test_decode_precision_is_fp32():
     """Probabilities and outputs of an fp16 + 2-bit cache to a few fp32 steps of the scores: capped scores keep the digits of
     scores far below their cap."""
